@@ -243,6 +243,151 @@ prr_status prr_repair(const prr_dims* dims, const void* q, const void* k_cache, 
                       hipStream_t stream);
 
 /* ---------------------------------------------------------------------------------
+ * Around the step: new tokens into the cache, prompts, whole caches, e4m3 caches.
+ * --------------------------------------------------------------------------------- */
+
+/* A batch of sequences whose caches share one pool of pages (dims.max_pages of them per KV
+ * head).  The calls above serve one sequence; these serve any number, one included.
+ *   n_seqs       sequences, 1..PRR_MAX_SEQS
+ *   total_q      rows of the packed tensors (queries, outputs), >= 1.  Rows at or behind
+ *                cu_q[n_seqs] belong to no sequence: they are not read, their outputs are left
+ *                as they were
+ *   max_q        no sequence has more new tokens than this
+ *   max_kv       no sequence has more tokens in its cache than this, 0..2^30; at most the
+ *                tokens of table_stride pages (without a table: of max_pages)
+ *   table_stride entries of a row of page_table (unused without one)
+ *   cu_q         device [n_seqs + 1] ascending int32 from 0: the new tokens of sequence s are
+ *                rows cu_q[s]..cu_q[s+1]; NULL = row s is the one new token of sequence s
+ *                (total_q >= n_seqs then)
+ *   kv_len       device [n_seqs] int32 tokens of each sequence, the new ones included: new
+ *                token i of q_len has position kv_len - q_len + i.  A negative position has
+ *                no place in the cache and sees no key
+ *   page_table   device [n_seqs][table_stride] int32 logical -> physical page, or NULL =
+ *                identity (n_seqs = 1).  Entries at or behind a sequence's last page are not
+ *                read.  An entry outside [0, max_pages) is never dereferenced.  No page may
+ *                hold two sequences' new tokens
+ * Device values beyond what max_q, max_kv and total_q say are cut to them. */
+typedef struct {
+  int32_t n_seqs;
+  int32_t total_q;
+  int32_t max_q;
+  int32_t max_kv;
+  int32_t table_stride;
+  const int32_t* cu_q;
+  const int32_t* kv_len;
+  const int32_t* page_table;
+} prr_batch;
+
+#define PRR_MAX_SEQS 4096
+
+/* What a cache holds.  PRR_KV_16: dims.dtype, [Hkv][max_pages][page_size][128].
+ * PRR_KV_E4M3: e4m3 codes (finite, no infinities: 448 the largest) of that layout, and one
+ * scale byte per row, [Hkv][max_pages][page_size] uint8: the row's numbers are
+ * code * 2^(byte - 127), byte in 1..254.  A power of two costs no accuracy (a float's relative
+ * step does not depend on its exponent) and reading back multiplies exactly. */
+#define PRR_KV_16 0
+#define PRR_KV_E4M3 1
+
+#define PRR_ROPE_HALF 0        /* pairs (i, i + rot_dim/2) */
+#define PRR_ROPE_INTERLEAVED 1 /* pairs (2i, 2i + 1) */
+
+#define PRR_ROPE_PLAIN 0
+#define PRR_ROPE_LINEAR 1
+#define PRR_ROPE_NTK 2
+#define PRR_ROPE_BY_PARTS 3
+#define PRR_ROPE_YARN 4
+
+/* Rotary frequencies (host code): freqs[i], radians per position of pair i < rot_dim/2, in
+ * float64, and the scale of the rotated values.  With w_i = base^(-2i/rot_dim), L =
+ * trained_len and f = factor:
+ *   PLAIN     w_i (factor, trained_len, lo, hi unused)
+ *   LINEAR    w_i / f
+ *   NTK       base replaced by base f^(rot_dim/(rot_dim-2)) (rot_dim >= 4)
+ *   BY_PARTS  g w_i + (1-g) w_i / f with g = clamp((L w_i/2pi - lo) / (hi - lo), 0, 1): pairs of
+ *             at least hi rotations over L positions keep their frequency, those of at most
+ *             lo are interpolated
+ *   YARN      the same with g falling linearly from 1 to 0 over the pair index between
+ *             max(floor(x(hi)), 0) and min(ceil(x(lo)), rot_dim - 1), x(r) = rot_dim
+ *             ln(L / 2pi r) / (2 ln base) the index of r rotations; scale = 0.1 ln f + 1
+ * *scale is 1 for the others.
+ * Errors: PRR_ERR_INVALID_ARG for rot_dim odd or outside [2, 128], base <= 1, factor < 1,
+ * trained_len < 1, not 0 < lo < hi, or a NULL pointer. */
+prr_status prr_rope_freqs(int32_t kind, int32_t rot_dim, double base, double factor, int32_t trained_len, double lo,
+                          double hi, double* freqs, float* scale);
+
+/* Rotary positions for new tokens, and their keys and values into the paged cache.
+ *   q, k, v      device, row t at q + t * q_stride etc. (strides in elements, multiples of 4;
+ *                within a row dense [Hq][128], [Hkv][128]): the three may be parts of one
+ *                tensor.  q NULL: no queries; k and v NULL: no cache
+ *   positions    device [total_q] int32 position for the rotation, or NULL = the token's
+ *                position in its sequence.  The place in the cache is always the latter
+ *   freqs        device [rot_dim/2] float64 radians per position (prr_rope_freqs), or NULL with
+ *                rot_dim = 0 (nothing is rotated)
+ *   rot_dim      channels [0, rot_dim) are rotated, a multiple of 8 in [0, 128]
+ *   layout       PRR_ROPE_HALF or PRR_ROPE_INTERLEAVED
+ *   rope_scale   factor of the rotated channels of q and k
+ *   q_out        device [total_q][Hq][128] dtype out, or NULL with q; q_out = q with a dense q
+ *                (in place) is allowed, any other overlap is not
+ *   kv_kind, k_cache, v_cache, k_scale, v_scale  the cache written (scales: E4M3 only)
+ * (a, b) -> (a c - b s, a s + b c) in float32 with c, s = rope_scale cos, sin of the angle, which
+ * is reduced in float64; one rounding to the 16-bit type or to e4m3.  E4M3: a row's scale is the
+ * least power of two 2^e, e >= -126, with max|x| <= 448 2^e; values beyond 15/16 of the 16-bit
+ * type's 2^16 or 2^128 are cut to that, so that every code reads back as a finite number; NaN stays
+ * NaN.  Tokens without a place in the cache are rotated but not stored.  The rest of the cache is
+ * left as it was.  No workspace. */
+prr_status prr_rope_append(const prr_dims* dims, const prr_batch* batch, const void* q, const void* k, const void* v,
+                           int64_t q_stride, int64_t k_stride, int64_t v_stride, const int32_t* positions,
+                           const double* freqs, int32_t rot_dim, int32_t layout, float rope_scale, void* q_out,
+                           int32_t kv_kind, void* k_cache, void* v_cache, uint8_t* k_scale, uint8_t* v_scale,
+                           hipStream_t stream);
+
+/* Pages of an e4m3 cache in 16 bits: logical pages [page_begin, page_end) of a sequence of
+ * num_tokens tokens.
+ *   page_table   device int32 logical -> physical page, or NULL = identity
+ *   k_out, v_out device [Hkv][page_end - page_begin][page_size][128] dtype out: a cache of its
+ *                own (identity table, max_pages = page_end - page_begin) for the calls above.
+ *                Tokens at or behind num_tokens, and pages whose entry is outside
+ *                [0, max_pages), are left as they were
+ *   num_tokens   >= 1; 0 <= page_begin <= page_end <= ceil(num_tokens / page_size)
+ * Exact but for numbers below the 16-bit type's smallest normal one, which are rounded to
+ * nearest. */
+prr_status prr_cache_read(const prr_dims* dims, const void* k_codes, const void* v_codes, const uint8_t* k_scale,
+                          const uint8_t* v_scale, const int32_t* page_table, int32_t num_tokens, int32_t page_begin,
+                          int32_t page_end, void* k_out, void* v_out, hipStream_t stream);
+
+/* Causal attention of new tokens over the cache that holds them and what came before (16-bit
+ * cache): the token at position p attends positions 0..p of its sequence.
+ *   q            device [total_q][Hq][128] dtype
+ *   out_o        device [total_q][Hq][128] dtype out
+ *   out_m, out_l device [total_q][Hq] float32 out (both or neither NULL)
+ * Weights are rounded to the 16-bit type for the product with the values, everything else is
+ * float32.  A token that sees no key gets the empty state.  A page-table entry out of range
+ * makes the results of its sequence unspecified.  Workspace: prr_prompt_workspace_size bytes,
+ * 256-byte aligned, contents of no account before and after (NULL if that is 0). */
+size_t prr_prompt_workspace_size(const prr_dims* dims, const prr_batch* batch);
+prr_status prr_prompt_attn(const prr_dims* dims, const prr_batch* batch, const void* q, const void* k_cache,
+                           const void* v_cache, void* out_o, float* out_m, float* out_l, void* workspace,
+                           size_t ws_bytes, hipStream_t stream);
+
+/* Attention of one token per sequence (cu_q NULL) over its whole cache, or over listed pages.
+ *   q            device [total_q][Hq][128] dtype
+ *   kv_kind, k_cache, v_cache, k_scale, v_scale  the cache (scales: E4M3 only)
+ *   pages        device [n_seqs][Hkv][cap] int32 logical pages (prr_score_topk's `selected` for
+ *                one sequence), distinct, or NULL = every page
+ *   page_count   device [n_seqs][Hkv] int32 entries of each list, or NULL with pages
+ *   cap          entries of a list, >= 1 (unused without lists)
+ *   out_o32      device [total_q][Hq][128] float32 out, out_o the same in dtype, out_m, out_l
+ *                [total_q][Hq] float32 out; out_o may be NULL
+ * List and table entries out of range are skipped.  The result does not depend on how the work is
+ * split but for rounding; the same call gives the same bits.  Workspace: as for prr_prompt_attn,
+ * prr_decode_workspace_size bytes (cap 0 = no lists). */
+size_t prr_decode_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t kv_kind, int32_t cap);
+prr_status prr_decode_attn(const prr_dims* dims, const prr_batch* batch, const void* q, int32_t kv_kind,
+                           const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
+                           const int32_t* pages, const int32_t* page_count, int32_t cap, float* out_o32, void* out_o,
+                           float* out_m, float* out_l, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------------
  * Decode-step runtime: one token over a stack of layers, launched natively.
  * --------------------------------------------------------------------------------- */
 

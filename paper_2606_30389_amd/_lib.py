@@ -32,6 +32,17 @@ PRR_MAX_CAP = 1024
 PRR_MAX_FORCED = 64
 PRR_STATIC_MAX_KV_HEADS = 256
 
+PRR_MAX_SEQS = 4096
+PRR_KV_16 = 0
+PRR_KV_E4M3 = 1
+PRR_ROPE_HALF = 0
+PRR_ROPE_INTERLEAVED = 1
+PRR_ROPE_PLAIN = 0
+PRR_ROPE_LINEAR = 1
+PRR_ROPE_NTK = 2
+PRR_ROPE_BY_PARTS = 3
+PRR_ROPE_YARN = 4
+
 PRR_SCHED_SERIAL = 0
 PRR_SCHED_TWO_STREAM = 1
 PRR_SCHED_PREFILL = 2
@@ -46,6 +57,8 @@ EXPORTED = (
     "prr_spec_attn", "prr_repair", "prr_merge_states", "prr_decode_step", "prr_calibrate",
     "prr_epoch_advance", "prr_pick_delta", "prr_score_topk_static", "prr_empty_launch", "prr_fused_grid",
     "prr_read_stream", "prr_stream_chain",
+    "prr_rope_freqs", "prr_rope_append", "prr_cache_read", "prr_prompt_workspace_size", "prr_prompt_attn",
+    "prr_decode_workspace_size", "prr_decode_attn",
 )
 
 
@@ -58,6 +71,11 @@ class PrrError(RuntimeError):
 class prr_dims(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int32) for name in
                 ("num_q_heads", "num_kv_heads", "head_dim", "page_size", "max_pages", "dtype", "meta_kind")]
+
+
+class prr_batch(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("n_seqs", "total_q", "max_q", "max_kv", "table_stride")] + [
+        ("cu_q", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
 
 
 class prr_layer_io(ctypes.Structure):
@@ -93,6 +111,9 @@ _I = ctypes.c_int32
 _F = ctypes.c_float
 _S = ctypes.c_size_t
 _DIMS = ctypes.POINTER(prr_dims)
+_BATCH = ctypes.POINTER(prr_batch)
+_L = ctypes.c_int64
+_D = ctypes.c_double
 
 _SIGS = {
     "prr_status_string": (ctypes.c_char_p, [_I]),
@@ -116,6 +137,13 @@ _SIGS = {
     "prr_read_stream": (_I, [_P, _S, _P, _I, _P]),
     "prr_stream_chain": (_I, [_I, _I, _P, _P]),
     "prr_fused_grid": (_I, [_DIMS, _P, _I]),
+    "prr_rope_freqs": (_I, [_I, _I, _D, _D, _I, _D, _D, _P, _P]),
+    "prr_rope_append": (_I, [_DIMS, _BATCH, _P, _P, _P, _L, _L, _L, _P, _P, _I, _I, _F, _P, _I, _P, _P, _P, _P, _P]),
+    "prr_cache_read": (_I, [_DIMS, _P, _P, _P, _P, _P, _I, _I, _I, _P, _P, _P]),
+    "prr_prompt_workspace_size": (_S, [_DIMS, _BATCH]),
+    "prr_prompt_attn": (_I, [_DIMS, _BATCH, _P, _P, _P, _P, _P, _P, _P, _S, _P]),
+    "prr_decode_workspace_size": (_S, [_DIMS, _BATCH, _I, _I]),
+    "prr_decode_attn": (_I, [_DIMS, _BATCH, _P, _I, _P, _P, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _S, _P]),
     "prr_pick_delta": (_I, [_P, _P, _P, _P, _I, _I, _I, _P, _P, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -275,6 +303,80 @@ def prr_pick_delta(rows, query_context, degree=2):
                                int(degree), ctypes.addressof(out), ctypes.addressof(out) + 4,
                                ctypes.addressof(out) + 8))
     return float(out[0]), float(out[1]), float(out[2])
+
+
+def make_batch(n_seqs, total_q, max_q, max_kv, cu_q, kv_len, page_table=None, table_stride=0):
+    """A prr_batch; it keeps the tensors that it points to."""
+    b = prr_batch(n_seqs, total_q, max_q, max_kv, table_stride, _ptr(cu_q), _ptr(kv_len), _ptr(page_table))
+    b.tensors = (cu_q, kv_len, page_table)
+    return b
+
+
+def _on_device(fn, like, stream, *args):
+    """fn(*args, stream) with `like`'s device current; stream None = that device's current stream."""
+    device = getattr(like, "device", None)
+    if device is None or device.type != "cuda":
+        return _check(fn(*args, _stream(stream)))
+    import torch
+    if device.index == torch.cuda.current_device():
+        return _check(fn(*args, torch._C._cuda_getCurrentRawStream(device.index) if stream is None else _stream(stream)))
+    with torch.cuda.device(device):
+        return _check(fn(*args, _stream(stream)))
+
+
+def _row_stride(x, heads, name):
+    """Elements between rows of x [rows][heads][128] (a tensor dense within a row), or of a dense array."""
+    if x is None or isinstance(x, int):
+        return heads * 128
+    if x.dim() != 3 or x.shape[1:] != (heads, 128) or x.stride()[1:] != (128, 1):
+        raise ValueError(f"{name} has shape {tuple(x.shape)}, strides {x.stride()}: expected [rows][{heads}][128], "
+                         "dense within a row")
+    return x.stride(0)
+
+
+def prr_rope_freqs(kind, rot_dim, base, factor=1.0, trained_len=1, lo=1.0, hi=32.0):
+    """Radians per position of each pair as a host float64 array, and the scale of the rotated values."""
+    import numpy as np
+    out = np.zeros(max(1, rot_dim // 2), dtype=np.float64)
+    scale = ctypes.c_float()
+    _check(_lib.prr_rope_freqs(kind, rot_dim, base, factor, trained_len, lo, hi, out.ctypes.data, ctypes.addressof(scale)))
+    return out, float(scale.value)
+
+
+def prr_rope_append(dims, batch, q, k, v, positions, freqs, rot_dim, layout, rope_scale, q_out, kv_kind, k_cache, v_cache,
+                    k_scale=None, v_scale=None, stream=None):
+    """q, k, v: tensors [rows][heads][128], dense within a row (their row strides are taken from them), or
+    addresses of dense arrays."""
+    _on_device(_lib.prr_rope_append, k_cache if q is None else q, stream, ctypes.byref(dims), ctypes.byref(batch), _ptr(q),
+               _ptr(k), _ptr(v), _row_stride(q, dims.num_q_heads, "q"), _row_stride(k, dims.num_kv_heads, "k"),
+               _row_stride(v, dims.num_kv_heads, "v"), _ptr(positions), _ptr(freqs), rot_dim, layout, rope_scale,
+               _ptr(q_out), kv_kind, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale))
+
+
+def prr_cache_read(dims, k_codes, v_codes, k_scale, v_scale, page_table, num_tokens, page_begin, page_end, k_out, v_out,
+                   stream=None):
+    _on_device(_lib.prr_cache_read, k_codes, stream, ctypes.byref(dims), _ptr(k_codes), _ptr(v_codes), _ptr(k_scale),
+               _ptr(v_scale), _ptr(page_table), num_tokens, page_begin, page_end, _ptr(k_out), _ptr(v_out))
+
+
+def prr_prompt_workspace_size(dims, batch) -> int:
+    return int(_lib.prr_prompt_workspace_size(ctypes.byref(dims), ctypes.byref(batch)))
+
+
+def prr_prompt_attn(dims, batch, q, k_cache, v_cache, out_o, out_m, out_l, workspace, ws_bytes, stream=None):
+    _on_device(_lib.prr_prompt_attn, q, stream, ctypes.byref(dims), ctypes.byref(batch), _ptr(q), _ptr(k_cache),
+               _ptr(v_cache), _ptr(out_o), _ptr(out_m), _ptr(out_l), _ptr(workspace), ws_bytes)
+
+
+def prr_decode_workspace_size(dims, batch, kv_kind, cap=0) -> int:
+    return int(_lib.prr_decode_workspace_size(ctypes.byref(dims), ctypes.byref(batch), kv_kind, cap))
+
+
+def prr_decode_attn(dims, batch, q, kv_kind, k_cache, v_cache, k_scale, v_scale, pages, page_count, cap, out_o32, out_o,
+                    out_m, out_l, workspace, ws_bytes, stream=None):
+    _on_device(_lib.prr_decode_attn, q, stream, ctypes.byref(dims), ctypes.byref(batch), _ptr(q), kv_kind, _ptr(k_cache),
+               _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(pages), _ptr(page_count), cap, _ptr(out_o32),
+               _ptr(out_o), _ptr(out_m), _ptr(out_l), _ptr(workspace), ws_bytes)
 
 
 def prr_empty_launch(grid, threads, stream=None):

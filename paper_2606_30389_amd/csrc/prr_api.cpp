@@ -238,6 +238,8 @@ prr_status api_fail(prr_status st, const char* fmt, ...) {
 }
 
 prr_status api_ok() { return ok(); }
+prr_status api_check_dims(const prr_dims* dims) { return check_dims(dims); }
+prr_status api_check_ptr(const void* p, const char* name, size_t align) { return check_ptr(p, name, align); }
 
 prr_status prepare_score(const prr_dims* dims, const void* q, const void* meta, int32_t num_pages, int32_t k_select,
                          const int32_t* forced, int32_t n_forced, int32_t forced_in_budget, float* scores,

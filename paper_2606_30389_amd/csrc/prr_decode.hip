@@ -1,0 +1,373 @@
+// Attention of one token per sequence over its whole cache or over listed pages.
+#include "prr_context.h"
+
+namespace prr {
+
+namespace {
+
+// The keys of a (sequence, KV head) are cut into tiles of 16 tokens (a tile lies in one page) and the
+// tiles into parts, one workgroup of eight waves each; wave w takes tiles w, w + 8, .. of its part with
+// an online softmax of its own, the next tile's loads issued before a tile is computed.  The wave
+// states are merged in LDS; with more than one part, by merge_parts_kernel over the parts.
+//
+// Matrix products and lane layout are those of the page-list attention (prr_sep.h, pv_tile): lane
+// 16j+n has the logits of tokens 4j..4j+3 for query head n and channels 32j + 8i + cb of its output.
+//
+// An e4m3 cache: codes are exact in either 16-bit type.  q.code is scaled by the key's power of two
+// in float32.  The value's power of two 2^ev joins the weight, p 2^ev = 2^(x + ev - y), y the largest
+// x + ev so far (x the logit in powers of two): every weight that counts is near 1, whatever the
+// scales, and the product runs in float16, whose two-term weights carry 22 bits (bfloat16's: 17).
+constexpr int kDecodeWaves = 8;
+constexpr int kDecodeThreads = kDecodeWaves * kWave;
+constexpr int kTile = 16;
+constexpr float kNoRef = -3e38f;  // nothing seen yet: 2^(kNoRef - anything later) = 0
+
+template <bool E4M3>
+struct TileData {
+  u32x4_t k[E4M3 ? 2 : 4];
+  u32x4_t v[4];  // E4M3: only .x, .y of each
+  uint32_t ks, vs;
+};
+
+template <bool BF16>
+__device__ __forceinline__ f32x4_t mfma16(const u32x4_t& a, const u32x4_t& b, f32x4_t c) {
+  if constexpr (BF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
+                                                   0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0,
+                                                  0, 0);
+  }
+}
+
+// Tile `row0` (first cache row) with `valid` tokens, 1..16; rows behind them repeat the last one.
+template <bool E4M3>
+__device__ __forceinline__ void load_tile(const CacheArgs& c, int64_t row0, int valid, TileData<E4M3>& d) {
+  const int lane = lane_id(), j = lane >> 4, m = lane & 15;
+  if constexpr (E4M3) {
+    const uint8_t* k = static_cast<const uint8_t*>(c.k) + (row0 + min(m, valid - 1)) * kHeadDim + 32 * j;
+    d.k[0] = *reinterpret_cast<const u32x4_t*>(k);
+    d.k[1] = *reinterpret_cast<const u32x4_t*>(k + 16);
+    const uint8_t* v = static_cast<const uint8_t*>(c.v) + row0 * kHeadDim + 8 * m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint2 w = *reinterpret_cast<const uint2*>(v + min(4 * j + i, valid - 1) * kHeadDim);
+      d.v[i][0] = w.x;
+      d.v[i][1] = w.y;
+    }
+    d.ks = *reinterpret_cast<const uint32_t*>(c.k_scale + row0 + 4 * j);
+    d.vs = *reinterpret_cast<const uint32_t*>(c.v_scale + row0 + 4 * j);
+  } else {
+    const uint16_t* k = static_cast<const uint16_t*>(c.k) + (row0 + min(m, valid - 1)) * kHeadDim + 32 * j;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) d.k[s] = reinterpret_cast<const u32x4_t*>(k)[s];
+    const uint16_t* v = static_cast<const uint16_t*>(c.v) + row0 * kHeadDim + 8 * m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) d.v[i] = *reinterpret_cast<const u32x4_t*>(v + min(4 * j + i, valid - 1) * kHeadDim);
+  }
+}
+
+// A wave's running state: per lane the head n = lane % 16.  mx the largest logit (unscaled q.k), ref
+// the exponent (powers of two) that l is relative to, yref the one of acc (E4M3; else ref), l this
+// lane's part of the sum.
+struct WaveState {
+  f32x4_t acc[8];
+  float mx, ref, yref, l;
+};
+
+template <bool BF16, bool E4M3>
+__device__ __forceinline__ void attend_tile(const TileData<E4M3>& d, const u32x4_t (&qf)[4], int valid, WaveState& st) {
+  const int j = lane_id() >> 4;
+  const float kNegInf = -__builtin_inff();
+  f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    if constexpr (E4M3) {
+      const uint32_t a = d.k[x >> 1][2 * (x & 1)], b = d.k[x >> 1][2 * (x & 1) + 1];
+      const u32x4_t kf = {unpack_codes<BF16, false>(a, 1.0f), unpack_codes<BF16, true>(a, 1.0f),
+                          unpack_codes<BF16, false>(b, 1.0f), unpack_codes<BF16, true>(b, 1.0f)};
+      s = mfma16<BF16>(kf, qf[x], s);
+    } else {
+      s = mfma16<BF16>(d.k[x], qf[x], s);
+    }
+  }
+  float y[4], top = kNegInf, ytop = kNegInf;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool live = 4 * j + i < valid;
+    if constexpr (E4M3) s[i] *= __uint_as_float(((d.ks >> (8 * i)) & 0xffu) << 23);
+    s[i] = live ? s[i] : kNegInf;
+    top = fmaxf(top, s[i]);
+    if constexpr (E4M3) {
+      y[i] = fmaf(s[i], kSoftmaxScale2, (float)(int)((d.vs >> (8 * i)) & 0xffu) - 127.0f);
+      ytop = fmaxf(ytop, y[i]);
+    }
+  }
+  st.mx = fmaxf(st.mx, max_rows(top));
+  const float ref = st.mx == kNegInf ? st.ref : st.mx * kSoftmaxScale2;
+  st.l *= exp2_hw(st.ref - ref);
+  float yref = ref;
+  if constexpr (E4M3) {
+    ytop = fmaxf(st.yref, max_rows(ytop));
+    yref = ytop == kNegInf ? st.yref : ytop;
+  }
+  if (__any(yref != st.yref)) {
+    const float alpha = exp2_hw(st.yref - yref);
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) st.acc[cb] *= alpha;
+  }
+  st.ref = ref;
+  st.yref = yref;
+  float w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float p = exp2_hw(fmaf(s[i], kSoftmaxScale2, -ref));
+    st.l += p;
+    w[i] = E4M3 ? exp2_hw(y[i] - yref) : p;
+  }
+  if constexpr (E4M3) {
+    u32x4_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v[i] = u32x4_t{unpack_codes<false, false>(d.v[i][0], 1.0f), unpack_codes<false, true>(d.v[i][0], 1.0f),
+                     unpack_codes<false, false>(d.v[i][1], 1.0f), unpack_codes<false, true>(d.v[i][1], 1.0f)};
+    pv_tile<false>(st.acc, v, w);
+  } else {
+    pv_tile<BF16>(st.acc, d.v, w);
+  }
+}
+
+// Tiles of (sequence s, KV head h).
+__device__ __forceinline__ int64_t key_tiles(const DecodeLaunch& a, int s, int h, int kv) {
+  if (!a.pages) return (kv + kTile - 1) / kTile;
+  const int n = min(max(a.page_count[(size_t)s * a.c.num_kv_heads + h], 0), a.cap);
+  return (int64_t)n << (a.c.page_shift - 4);
+}
+
+// head g of a (sequence, KV head): o of four channels from c4 on, the largest logit (unscaled), the sum
+template <bool BF16>
+__device__ __forceinline__ void store_row(const DecodeLaunch& a, int64_t row, int c4, float4 o, float mx, float l) {
+  *reinterpret_cast<float4*>(a.out_o32 + row * kHeadDim + c4) = o;
+  if (a.out_o)
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out_o) + row * kHeadDim + c4) =
+        make_uint2(pack2<BF16>(o.x, o.y), pack2<BF16>(o.z, o.w));
+  if (c4 == 0) {
+    a.out_m[row] = mx * kSoftmaxScale;
+    a.out_l[row] = l;
+  }
+}
+
+struct DecodeLds {
+  float o[kDecodeWaves][16][kHeadDim + 4];
+  float m[kDecodeWaves][16], l[kDecodeWaves][16];
+};
+
+template <bool BF16, bool E4M3>
+__global__ __launch_bounds__(kDecodeThreads) void decode_kernel(const DecodeLaunch a) {
+  __shared__ __align__(16) DecodeLds S;
+  const int t = threadIdx.x, lane = lane_id(), w = __builtin_amdgcn_readfirstlane(t / kWave);
+  const int j = lane >> 4, n = lane & 15;
+  const int part = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
+  const int G = a.group;
+  const float kNegInf = -__builtin_inff();
+  const int kv = min(max(a.b.kv_len[s], 0), a.b.max_kv);
+  const int64_t tiles = key_tiles(a, s, h, kv);
+  const int64_t begin = (int64_t)part * a.tiles_per_split;
+  if (part > 0 && begin >= tiles) return;  // (a part without tiles is not merged)
+  const int count = (int)min(tiles - begin, (int64_t)a.tiles_per_split);
+
+  u32x4_t qf[4];
+  const uint16_t* q = static_cast<const uint16_t*>(a.q) + ((int64_t)(s * a.c.num_kv_heads + h) * G + min(n, G - 1)) * kHeadDim;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) qf[x] = reinterpret_cast<const u32x4_t*>(q + 32 * j)[x];
+
+  WaveState st;
+#pragma unroll
+  for (int cb = 0; cb < 8; ++cb) st.acc[cb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  st.mx = kNegInf;
+  st.ref = st.yref = kNoRef;
+  st.l = 0.0f;
+
+  const int sh = a.c.page_shift - 4;  // log2 of the tiles of a page
+  const int64_t head_row = (int64_t)h * a.c.max_pages * a.c.page_size;
+  const int mine = (count - w + kDecodeWaves - 1) / kDecodeWaves;  // tiles w, w + 8, .. of the part
+  for (int i0 = 0; i0 < mine; i0 += kWave) {
+    // where the wave's next 64 tiles lie: lane i looks tile i0 + i up
+    int64_t my_row = 0;
+    int my_valid = 0;
+    if (i0 + lane < mine) {
+      const int64_t x = begin + w + (int64_t)kDecodeWaves * (i0 + lane);
+      const int sub = (int)x & ((1 << sh) - 1);
+      int lp = (int)(x >> sh);
+      if (a.pages) lp = a.pages[((size_t)s * a.c.num_kv_heads + h) * a.cap + lp];
+      const int64_t tok = ((int64_t)lp << a.c.page_shift) + sub * kTile;
+      if (lp >= 0 && tok < kv) {
+        const int phys = phys_page(a.b.page_table, a.b.table_stride, a.c.max_pages, s, lp);
+        if (phys >= 0) {
+          my_valid = (int)min(kv - tok, (int64_t)kTile);
+          my_row = head_row + ((int64_t)phys << a.c.page_shift) + sub * kTile;
+        }
+      }
+    }
+    // the valid tiles, in order, the next one's loads ahead of a tile's products
+    uint64_t todo = __ballot(my_valid > 0);
+    if (!todo) continue;
+    const auto take = [&](int& valid, int64_t& row) {
+      const int i = __builtin_ctzll(todo);
+      todo &= todo - 1;
+      valid = __builtin_amdgcn_readlane(my_valid, i);
+      row = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(my_row >> 32), i) << 32) |
+                      (uint32_t)__builtin_amdgcn_readlane((int)my_row, i));
+    };
+    TileData<E4M3> d0, d1;
+    int v0, v1;
+    int64_t row;
+    take(v0, row);
+    load_tile<E4M3>(a.c, row, v0, d0);
+    for (;;) {
+      const bool more = todo != 0;
+      if (more) {
+        take(v1, row);
+        load_tile<E4M3>(a.c, row, v1, d1);
+      }
+      attend_tile<BF16, E4M3>(d0, qf, v0, st);
+      if (!more) break;
+      const bool more2 = todo != 0;
+      if (more2) {
+        take(v0, row);
+        load_tile<E4M3>(a.c, row, v0, d0);
+      }
+      attend_tile<BF16, E4M3>(d1, qf, v1, st);
+      if (!more2) break;
+    }
+  }
+
+  // the wave's state, normalised: o = acc 2^(yref - ref) / l
+  const float l = sum_rows(st.l);
+  const float norm = l > 0.0f || l != l ? exp2_hw(E4M3 ? st.yref - st.ref : 0.0f) / l : 0.0f;
+  // l relative to the logit itself, not to its rounded product with the scale
+  const float exact = st.mx == kNegInf ? 0.0f : l * exp2_hw(-fmaf(st.mx, kSoftmaxScale2, -st.ref));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int c = 0; c < 8; c += 4) {
+      const float4 o = make_float4(st.acc[c][i] * norm, st.acc[c + 1][i] * norm, st.acc[c + 2][i] * norm, st.acc[c + 3][i] * norm);
+      *reinterpret_cast<float4*>(&S.o[w][n][32 * j + 8 * i + c]) = o;
+    }
+  }
+  if (j == 0) {
+    S.m[w][n] = st.mx;
+    S.l[w][n] = exact;
+  }
+  __syncthreads();
+  // 32 threads per head, four channels each
+  const int g = t >> 5, c4 = (t & 31) * 4;
+  if (g >= G) return;
+  float mx = kNegInf;
+#pragma unroll
+  for (int x = 0; x < kDecodeWaves; ++x) mx = fmaxf(mx, S.m[x][g]);
+  float sum = 0.0f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int x = 0; x < kDecodeWaves; ++x) {
+    const float m = S.m[x][g];
+    const float f = m == kNegInf ? 0.0f : S.l[x][g] * exp2_hw((m - mx) * kSoftmaxScale2);
+    if (f == 0.0f) continue;
+    const float4 y = *reinterpret_cast<const float4*>(&S.o[x][g][c4]);
+    sum += f;
+    o.x += f * y.x;
+    o.y += f * y.y;
+    o.z += f * y.z;
+    o.w += f * y.w;
+  }
+  const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+  o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  if (a.nsplit == 1) {
+    store_row<BF16>(a, (int64_t)(s * a.c.num_kv_heads + h) * G + g, c4, o, mx, sum);
+  } else {
+    const int64_t at = ((int64_t)(s * a.c.num_kv_heads + h) * a.nsplit + part) * G + g;
+    *reinterpret_cast<float4*>(a.part_o + at * kHeadDim + c4) = o;
+    if (c4 == 0) {
+      a.part_ml[2 * at] = mx;
+      a.part_ml[2 * at + 1] = sum;
+    }
+  }
+}
+
+// The parts of one query head of one sequence: eight groups of 32 threads take every eighth part,
+// four channels a thread; the groups are added in LDS.
+template <bool BF16>
+__global__ __launch_bounds__(256) void merge_parts_kernel(const DecodeLaunch a) {
+  __shared__ float so[8][kHeadDim], sl[8], sm[4];
+  const int t = threadIdx.x, grp = t >> 5, c4 = (t & 31) * 4;
+  const int g = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
+  const float kNegInf = -__builtin_inff();
+  const int kv = min(max(a.b.kv_len[s], 0), a.b.max_kv);
+  const int64_t tiles = key_tiles(a, s, h, kv);
+  const int parts = (int)min((tiles + a.tiles_per_split - 1) / a.tiles_per_split, (int64_t)a.nsplit);
+  const int64_t base = (int64_t)(s * a.c.num_kv_heads + h) * a.nsplit;
+  const auto at = [&](int p) { return (base + p) * a.group + g; };
+  float mx = kNegInf;
+  for (int p = t; p < parts; p += 256) mx = fmaxf(mx, a.part_ml[2 * at(p)]);
+  mx = wave_max(mx);
+  if (lane_id() == 0) sm[t / kWave] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  float sum = 0.0f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p = grp; p < parts; p += 8) {
+    const float m = a.part_ml[2 * at(p)], l = a.part_ml[2 * at(p) + 1];
+    const float4 y = *reinterpret_cast<const float4*>(a.part_o + at(p) * kHeadDim + c4);
+    const float f = m == kNegInf ? 0.0f : l * exp2_hw((m - mx) * kSoftmaxScale2);
+    if (f != 0.0f) {
+      sum += f;
+      o.x += f * y.x;
+      o.y += f * y.y;
+      o.z += f * y.z;
+      o.w += f * y.w;
+    }
+  }
+  *reinterpret_cast<float4*>(&so[grp][c4]) = o;
+  if (c4 == 0) sl[grp] = sum;
+  __syncthreads();
+  if (grp) return;
+  sum = 0.0f;
+  o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    const float4 y = *reinterpret_cast<const float4*>(&so[x][c4]);
+    sum += sl[x];
+    o.x += y.x;
+    o.y += y.y;
+    o.z += y.z;
+    o.w += y.w;
+  }
+  const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+  store_row<BF16>(a, (int64_t)(s * a.c.num_kv_heads + h) * a.group + g, c4,
+                  make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), mx, sum);
+}
+
+}  // namespace
+
+void plan_decode(DecodeLaunch& a) {
+  const int64_t most = a.cap > 0 ? (int64_t)a.cap * a.c.page_size : a.b.max_kv;
+  const int64_t tiles = max((most + kTile - 1) / kTile, (int64_t)1);
+  const int64_t units = (int64_t)a.b.n_seqs * a.c.num_kv_heads;
+  // two workgroups per CU, but no wave without a tile
+  const int64_t want = min(max((int64_t)512 / units, (int64_t)1), (tiles + kDecodeWaves - 1) / kDecodeWaves);
+  const int64_t per = ((tiles + want - 1) / want + kDecodeWaves - 1) / kDecodeWaves * kDecodeWaves;
+  a.tiles_per_split = (int)per;
+  a.nsplit = (int)((tiles + per - 1) / per);
+}
+
+hipError_t launch_decode(const DecodeLaunch& a, hipStream_t stream) {
+  const void* f = a.bf16 ? (a.e4m3 ? (const void*)decode_kernel<true, true> : (const void*)decode_kernel<true, false>)
+                         : (a.e4m3 ? (const void*)decode_kernel<false, true> : (const void*)decode_kernel<false, false>);
+  const hipError_t e =
+      launch_one(f, dim3(a.nsplit, a.c.num_kv_heads, a.b.n_seqs), kDecodeThreads, stream, a);
+  if (e != hipSuccess || a.nsplit == 1) return e;
+  return launch_one(a.bf16 ? (const void*)merge_parts_kernel<true> : (const void*)merge_parts_kernel<false>,
+                    dim3(a.group, a.c.num_kv_heads, a.b.n_seqs), 256, stream, a);
+}
+
+}  // namespace prr

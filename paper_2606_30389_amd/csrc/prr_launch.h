@@ -196,6 +196,8 @@ prr_status prepare_score(const prr_dims* dims, const void* q, const void* meta, 
                          int32_t* selected, int32_t* selected_count, int32_t cap, ScoreLaunch& a);
 prr_status api_fail(prr_status st, const char* fmt, ...);
 prr_status api_ok();
+prr_status api_check_dims(const prr_dims* dims);
+prr_status api_check_ptr(const void* p, const char* name, size_t align);
 
 hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t stream);
 hipError_t launch_empty(int grid, int threads, hipStream_t stream);
