@@ -5,20 +5,24 @@ namespace prr {
 
 namespace {
 
-// The keys of a (sequence, KV head) are cut into tiles of 16 tokens (a tile lies in one page) and the
-// tiles into parts, one workgroup of eight waves each; wave w takes tiles w, w + 8, .. of its part with
-// an online softmax of its own, the next tile's loads issued before a tile is computed.  The wave
+// The keys of a (sequence, KV head) are cut into tiles of 16 tokens, the tiles into runs of eight, and the
+// runs are dealt out to the parts, one workgroup of eight waves each, so that all workgroups read one
+// moving window of the cache (parts of consecutive tokens: 32 sequences of up to 16K tokens 250 us, dealt
+// out 244; 64 MiB read so by the bare loads 11.7 us, by 2048 workgroups 13.4).  Wave w takes tile w of
+// each run with an online softmax of its own, the next tile's loads issued before a tile is computed (more
+// in flight is no faster: the loads alone take 18.7 us of the 19.3 of 2 x 131072 tokens).  The wave
 // states are merged in LDS; with more than one part, by merge_parts_kernel over the parts.
 //
-// Matrix products and lane layout are those of the page-list attention (prr_sep.h, pv_tile): lane
-// 16j+n has the logits of tokens 4j..4j+3 for query head n and channels 32j + 8i + cb of its output.
+// Matrix products are those of the page-list attention (prr_sep.h, pv_tile): lane 16j+n has the logits of
+// tokens 4j..4j+3 for query head n and channels 32j + 8i + cb of its output.  A key row's 16-byte
+// pieces go to the four lanes of a load instruction in order, 64 bytes of a row at a time (64 bytes of a
+// row to one lane, a load each 16: 271 us where this takes 250).
 //
 // An e4m3 cache: codes are exact in either 16-bit type.  q.code is scaled by the key's power of two
 // in float32.  The value's power of two 2^ev joins the weight, p 2^ev = 2^(x + ev - y), y the largest
 // x + ev so far (x the logit in powers of two): every weight that counts is near 1, whatever the
 // scales, and the product runs in float16, whose two-term weights carry 22 bits (bfloat16's: 17).
-constexpr int kDecodeWaves = 8;
-constexpr int kDecodeThreads = kDecodeWaves * kWave;
+constexpr int NW = 8;  // waves of a workgroup
 constexpr int kTile = 16;
 constexpr float kNoRef = -3e38f;  // nothing seen yet: 2^(kNoRef - anything later) = 0
 
@@ -45,9 +49,9 @@ template <bool E4M3>
 __device__ __forceinline__ void load_tile(const CacheArgs& c, int64_t row0, int valid, TileData<E4M3>& d) {
   const int lane = lane_id(), j = lane >> 4, m = lane & 15;
   if constexpr (E4M3) {
-    const uint8_t* k = static_cast<const uint8_t*>(c.k) + (row0 + min(m, valid - 1)) * kHeadDim + 32 * j;
+    const uint8_t* k = static_cast<const uint8_t*>(c.k) + (row0 + min(m, valid - 1)) * kHeadDim + 16 * j;
     d.k[0] = *reinterpret_cast<const u32x4_t*>(k);
-    d.k[1] = *reinterpret_cast<const u32x4_t*>(k + 16);
+    d.k[1] = *reinterpret_cast<const u32x4_t*>(k + 64);
     const uint8_t* v = static_cast<const uint8_t*>(c.v) + row0 * kHeadDim + 8 * m;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -58,9 +62,9 @@ __device__ __forceinline__ void load_tile(const CacheArgs& c, int64_t row0, int 
     d.ks = *reinterpret_cast<const uint32_t*>(c.k_scale + row0 + 4 * j);
     d.vs = *reinterpret_cast<const uint32_t*>(c.v_scale + row0 + 4 * j);
   } else {
-    const uint16_t* k = static_cast<const uint16_t*>(c.k) + (row0 + min(m, valid - 1)) * kHeadDim + 32 * j;
+    const uint16_t* k = static_cast<const uint16_t*>(c.k) + (row0 + min(m, valid - 1)) * kHeadDim + 8 * j;
 #pragma unroll
-    for (int s = 0; s < 4; ++s) d.k[s] = reinterpret_cast<const u32x4_t*>(k)[s];
+    for (int s = 0; s < 4; ++s) d.k[s] = *reinterpret_cast<const u32x4_t*>(k + 32 * s);
     const uint16_t* v = static_cast<const uint16_t*>(c.v) + row0 * kHeadDim + 8 * m;
 #pragma unroll
     for (int i = 0; i < 4; ++i) d.v[i] = *reinterpret_cast<const u32x4_t*>(v + min(4 * j + i, valid - 1) * kHeadDim);
@@ -138,10 +142,12 @@ __device__ __forceinline__ void attend_tile(const TileData<E4M3>& d, const u32x4
 }
 
 // Tiles of (sequence s, KV head h).
-__device__ __forceinline__ int64_t key_tiles(const DecodeLaunch& a, int s, int h, int kv) {
+__device__ __forceinline__ int key_tiles(const DecodeLaunch& a, int s, int h, int kv) {
   if (!a.pages) return (kv + kTile - 1) / kTile;
-  const int n = min(max(a.page_count[(size_t)s * a.c.num_kv_heads + h], 0), a.cap);
-  return (int64_t)n << (a.c.page_shift - 4);
+  return min(max(a.page_count[(size_t)s * a.c.num_kv_heads + h], 0), a.cap) << (a.c.page_shift - 4);
+}
+__device__ __forceinline__ int parts_of(const DecodeLaunch& a, int tiles) {
+  return min((tiles + a.tiles_per_split - 1) / a.tiles_per_split, a.nsplit);
 }
 
 // head g of a (sequence, KV head): o of four channels from c4 on, the largest logit (unscaled), the sum
@@ -158,12 +164,12 @@ __device__ __forceinline__ void store_row(const DecodeLaunch& a, int64_t row, in
 }
 
 struct DecodeLds {
-  float o[kDecodeWaves][16][kHeadDim + 4];
-  float m[kDecodeWaves][16], l[kDecodeWaves][16];
+  float o[NW][16][kHeadDim + 4];
+  float m[NW][16], l[NW][16];
 };
 
 template <bool BF16, bool E4M3>
-__global__ __launch_bounds__(kDecodeThreads) void decode_kernel(const DecodeLaunch a) {
+__global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a) {
   __shared__ __align__(16) DecodeLds S;
   const int t = threadIdx.x, lane = lane_id(), w = __builtin_amdgcn_readfirstlane(t / kWave);
   const int j = lane >> 4, n = lane & 15;
@@ -171,15 +177,14 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_kernel(const DecodeLaun
   const int G = a.group;
   const float kNegInf = -__builtin_inff();
   const int kv = min(max(a.b.kv_len[s], 0), a.b.max_kv);
-  const int64_t tiles = key_tiles(a, s, h, kv);
-  const int64_t begin = (int64_t)part * a.tiles_per_split;
-  if (part > 0 && begin >= tiles) return;  // (a part without tiles is not merged)
-  const int count = (int)min(tiles - begin, (int64_t)a.tiles_per_split);
+  const int tiles = key_tiles(a, s, h, kv), parts = max(parts_of(a, tiles), 1);
+  if (part >= parts) return;
 
   u32x4_t qf[4];
   const uint16_t* q = static_cast<const uint16_t*>(a.q) + ((int64_t)(s * a.c.num_kv_heads + h) * G + min(n, G - 1)) * kHeadDim;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) qf[x] = reinterpret_cast<const u32x4_t*>(q + 32 * j)[x];
+  for (int x = 0; x < 4; ++x)
+    qf[x] = *reinterpret_cast<const u32x4_t*>(q + (E4M3 ? 64 * (x >> 1) + 16 * j + 8 * (x & 1) : 32 * x + 8 * j));
 
   WaveState st;
 #pragma unroll
@@ -190,15 +195,17 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_kernel(const DecodeLaun
 
   const int sh = a.c.page_shift - 4;  // log2 of the tiles of a page
   const int64_t head_row = (int64_t)h * a.c.max_pages * a.c.page_size;
-  const int mine = (count - w + kDecodeWaves - 1) / kDecodeWaves;  // tiles w, w + 8, .. of the part
+  // tile w of the part's runs of NW tiles, every parts-th run
+  const int step = parts * NW, first = part * NW + w;
+  const int mine = (tiles - first + step - 1) / step;
   for (int i0 = 0; i0 < mine; i0 += kWave) {
     // where the wave's next 64 tiles lie: lane i looks tile i0 + i up
     int64_t my_row = 0;
     int my_valid = 0;
     if (i0 + lane < mine) {
-      const int64_t x = begin + w + (int64_t)kDecodeWaves * (i0 + lane);
-      const int sub = (int)x & ((1 << sh) - 1);
-      int lp = (int)(x >> sh);
+      const int x = first + step * (i0 + lane);
+      const int sub = x & ((1 << sh) - 1);
+      int lp = x >> sh;
       if (a.pages) lp = a.pages[((size_t)s * a.c.num_kv_heads + h) * a.cap + lp];
       const int64_t tok = ((int64_t)lp << a.c.page_shift) + sub * kTile;
       if (lp >= 0 && tok < kv) {
@@ -219,26 +226,25 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_kernel(const DecodeLaun
       row = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(my_row >> 32), i) << 32) |
                       (uint32_t)__builtin_amdgcn_readlane((int)my_row, i));
     };
-    TileData<E4M3> d0, d1;
-    int v0, v1;
-    int64_t row;
-    take(v0, row);
-    load_tile<E4M3>(a.c, row, v0, d0);
-    for (;;) {
-      const bool more = todo != 0;
-      if (more) {
-        take(v1, row);
-        load_tile<E4M3>(a.c, row, v1, d1);
+    constexpr int NB = 2;  // tiles in flight per wave
+    TileData<E4M3> d[NB];
+    int valid[NB];
+    const auto next = [&](int x) {
+      valid[x] = 0;
+      if (!todo) return;
+      int64_t row;
+      take(valid[x], row);
+      load_tile<E4M3>(a.c, row, valid[x], d[x]);
+    };
+#pragma unroll
+    for (int x = 0; x < NB; ++x) next(x);
+    while (valid[0]) {
+#pragma unroll
+      for (int x = 0; x < NB; ++x) {
+        if (!valid[x]) break;
+        attend_tile<BF16, E4M3>(d[x], qf, valid[x], st);
+        next(x);
       }
-      attend_tile<BF16, E4M3>(d0, qf, v0, st);
-      if (!more) break;
-      const bool more2 = todo != 0;
-      if (more2) {
-        take(v0, row);
-        load_tile<E4M3>(a.c, row, v0, d0);
-      }
-      attend_tile<BF16, E4M3>(d1, qf, v1, st);
-      if (!more2) break;
     }
   }
 
@@ -261,90 +267,113 @@ __global__ __launch_bounds__(kDecodeThreads) void decode_kernel(const DecodeLaun
   }
   __syncthreads();
   // 32 threads per head, four channels each
-  const int g = t >> 5, c4 = (t & 31) * 4;
-  if (g >= G) return;
-  float mx = kNegInf;
+  const int c4 = (t & 31) * 4;
+  for (int g = t >> 5; g < G; g += 2 * NW) {
+    float mx = kNegInf;
 #pragma unroll
-  for (int x = 0; x < kDecodeWaves; ++x) mx = fmaxf(mx, S.m[x][g]);
-  float sum = 0.0f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int x = 0; x < NW; ++x) mx = fmaxf(mx, S.m[x][g]);
+    float sum = 0.0f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int x = 0; x < kDecodeWaves; ++x) {
-    const float m = S.m[x][g];
-    const float f = m == kNegInf ? 0.0f : S.l[x][g] * exp2_hw((m - mx) * kSoftmaxScale2);
-    if (f == 0.0f) continue;
-    const float4 y = *reinterpret_cast<const float4*>(&S.o[x][g][c4]);
-    sum += f;
-    o.x += f * y.x;
-    o.y += f * y.y;
-    o.z += f * y.z;
-    o.w += f * y.w;
-  }
-  const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-  o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  if (a.nsplit == 1) {
-    store_row<BF16>(a, (int64_t)(s * a.c.num_kv_heads + h) * G + g, c4, o, mx, sum);
-  } else {
-    const int64_t at = ((int64_t)(s * a.c.num_kv_heads + h) * a.nsplit + part) * G + g;
-    *reinterpret_cast<float4*>(a.part_o + at * kHeadDim + c4) = o;
-    if (c4 == 0) {
-      a.part_ml[2 * at] = mx;
-      a.part_ml[2 * at + 1] = sum;
-    }
-  }
-}
-
-// The parts of one query head of one sequence: eight groups of 32 threads take every eighth part,
-// four channels a thread; the groups are added in LDS.
-template <bool BF16>
-__global__ __launch_bounds__(256) void merge_parts_kernel(const DecodeLaunch a) {
-  __shared__ float so[8][kHeadDim], sl[8], sm[4];
-  const int t = threadIdx.x, grp = t >> 5, c4 = (t & 31) * 4;
-  const int g = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
-  const float kNegInf = -__builtin_inff();
-  const int kv = min(max(a.b.kv_len[s], 0), a.b.max_kv);
-  const int64_t tiles = key_tiles(a, s, h, kv);
-  const int parts = (int)min((tiles + a.tiles_per_split - 1) / a.tiles_per_split, (int64_t)a.nsplit);
-  const int64_t base = (int64_t)(s * a.c.num_kv_heads + h) * a.nsplit;
-  const auto at = [&](int p) { return (base + p) * a.group + g; };
-  float mx = kNegInf;
-  for (int p = t; p < parts; p += 256) mx = fmaxf(mx, a.part_ml[2 * at(p)]);
-  mx = wave_max(mx);
-  if (lane_id() == 0) sm[t / kWave] = mx;
-  __syncthreads();
-  mx = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  float sum = 0.0f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int p = grp; p < parts; p += 8) {
-    const float m = a.part_ml[2 * at(p)], l = a.part_ml[2 * at(p) + 1];
-    const float4 y = *reinterpret_cast<const float4*>(a.part_o + at(p) * kHeadDim + c4);
-    const float f = m == kNegInf ? 0.0f : l * exp2_hw((m - mx) * kSoftmaxScale2);
-    if (f != 0.0f) {
+    for (int x = 0; x < NW; ++x) {
+      const float m = S.m[x][g];
+      const float f = m == kNegInf ? 0.0f : S.l[x][g] * exp2_hw((m - mx) * kSoftmaxScale2);
+      if (f == 0.0f) continue;
+      const float4 y = *reinterpret_cast<const float4*>(&S.o[x][g][c4]);
       sum += f;
       o.x += f * y.x;
       o.y += f * y.y;
       o.z += f * y.z;
       o.w += f * y.w;
     }
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+    o = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (a.nsplit == 1) {
+      store_row<BF16>(a, (int64_t)(s * a.c.num_kv_heads + h) * G + g, c4, o, mx, sum);
+    } else {
+      const int64_t at = ((int64_t)(s * a.c.num_kv_heads + h) * a.nsplit + part) * G + g;
+      *reinterpret_cast<float4*>(a.part_o + at * kHeadDim + c4) = o;
+      if (c4 == 0) {
+        a.part_ml[2 * at] = mx;
+        a.part_ml[2 * at + 1] = sum;
+      }
+    }
   }
-  *reinterpret_cast<float4*>(&so[grp][c4]) = o;
-  if (c4 == 0) sl[grp] = sum;
-  __syncthreads();
-  if (grp) return;
-  sum = 0.0f;
-  o = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+// The parts of one query head of one sequence, 32 of the 128 channels: eight threads take a part (four
+// channels each), 32 parts at a time; the first 128 parts' rows are loaded before their weights are
+// known.
+constexpr int kMergeEarly = 4;
+
+template <bool BF16>
+__global__ __launch_bounds__(256) void merge_parts_kernel(const DecodeLaunch a) {
+  __shared__ float so[4][32], sl[4], sm[4];
+  const int t = threadIdx.x, slot = t >> 3, w = t / kWave;
+  const int g = blockIdx.x >> 2, c4 = (blockIdx.x & 3) * 32 + (t & 7) * 4, h = blockIdx.y, s = blockIdx.z;
+  const float kNegInf = -__builtin_inff();
+  const int kv = min(max(a.b.kv_len[s], 0), a.b.max_kv);
+  const int parts = parts_of(a, key_tiles(a, s, h, kv));
+  const int64_t base = (int64_t)(s * a.c.num_kv_heads + h) * a.nsplit;
+  const auto at = [&](int p) { return (base + p) * a.group + g; };
+  float4 y[kMergeEarly];
+  float2 ml[kMergeEarly];
 #pragma unroll
-  for (int x = 0; x < 8; ++x) {
-    const float4 y = *reinterpret_cast<const float4*>(&so[x][c4]);
-    sum += sl[x];
-    o.x += y.x;
-    o.y += y.y;
-    o.z += y.z;
-    o.w += y.w;
+  for (int x = 0; x < kMergeEarly; ++x) {
+    const int p = slot + 32 * x;
+    y[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+    ml[x] = make_float2(kNegInf, 0.f);
+    if (p < parts) {
+      ml[x] = *reinterpret_cast<const float2*>(a.part_ml + 2 * at(p));
+      y[x] = *reinterpret_cast<const float4*>(a.part_o + at(p) * kHeadDim + c4);
+    }
   }
+  float mx = kNegInf;
+#pragma unroll
+  for (int x = 0; x < kMergeEarly; ++x) mx = fmaxf(mx, ml[x].x);
+  for (int p = 32 * kMergeEarly + t; p < parts; p += 256) mx = fmaxf(mx, a.part_ml[2 * at(p)]);
+  mx = wave_max(mx);
+  if (lane_id() == 0) sm[w] = mx;
+  __syncthreads();
+  mx = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  float sum = 0.0f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  const auto add = [&](const float2& st, const float4& v) {
+    const float f = st.x == kNegInf ? 0.0f : st.y * exp2_hw((st.x - mx) * kSoftmaxScale2);
+    if (f != 0.0f) {
+      sum += f;
+      o.x += f * v.x;
+      o.y += f * v.y;
+      o.z += f * v.z;
+      o.w += f * v.w;
+    }
+  };
+#pragma unroll
+  for (int x = 0; x < kMergeEarly; ++x) add(ml[x], y[x]);
+  for (int p = slot + 32 * kMergeEarly; p < parts; p += 32)
+    add(*reinterpret_cast<const float2*>(a.part_ml + 2 * at(p)),
+        *reinterpret_cast<const float4*>(a.part_o + at(p) * kHeadDim + c4));
+  // the eight parts of a wave (lanes 8 apart), then the four waves
+#pragma unroll
+  for (int x = 8; x < kWave; x *= 2) {
+    sum += __shfl_xor(sum, x);
+    o.x += __shfl_xor(o.x, x);
+    o.y += __shfl_xor(o.y, x);
+    o.z += __shfl_xor(o.z, x);
+    o.w += __shfl_xor(o.w, x);
+  }
+  if (lane_id() < 8) {
+    *reinterpret_cast<float4*>(&so[w][4 * lane_id()]) = o;
+    sl[w] = sum;
+  }
+  __syncthreads();
+  if (t >= 8) return;
+  sum = (sl[0] + sl[1]) + (sl[2] + sl[3]);
   const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-  store_row<BF16>(a, (int64_t)(s * a.c.num_kv_heads + h) * a.group + g, c4,
-                  make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv), mx, sum);
+  float r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = ((so[0][4 * t + i] + so[1][4 * t + i]) + (so[2][4 * t + i] + so[3][4 * t + i])) * inv;
+  store_row<BF16>(a, (int64_t)(s * a.c.num_kv_heads + h) * a.group + g, c4, make_float4(r[0], r[1], r[2], r[3]), mx, sum);
 }
 
 }  // namespace
@@ -353,9 +382,13 @@ void plan_decode(DecodeLaunch& a) {
   const int64_t most = a.cap > 0 ? (int64_t)a.cap * a.c.page_size : a.b.max_kv;
   const int64_t tiles = max((most + kTile - 1) / kTile, (int64_t)1);
   const int64_t units = (int64_t)a.b.n_seqs * a.c.num_kv_heads;
-  // two workgroups per CU, but no wave without a tile
-  const int64_t want = min(max((int64_t)512 / units, (int64_t)1), (tiles + kDecodeWaves - 1) / kDecodeWaves);
-  const int64_t per = ((tiles + want - 1) / want + kDecodeWaves - 1) / kDecodeWaves * kDecodeWaves;
+  // Parts of 64 tiles (eight a wave: less, and starting and merging parts outweighs them; 512 parts of
+  // 32 tiles for 2 x 8192: 27.8 us, 256 of 64: 21.0) or of the share of 512 workgroups, two a CU; where that
+  // leaves CUs idle, as many parts as CUs, of a tile a wave at least.
+  const int64_t all = tiles * units;
+  int64_t per = max((int64_t)64, (all + 511) / 512);
+  if (all < 64 * 256) per = (all + 255) / 256;
+  per = (min(per, tiles) + NW - 1) / NW * NW;
   a.tiles_per_split = (int)per;
   a.nsplit = (int)((tiles + per - 1) / per);
 }
@@ -363,11 +396,10 @@ void plan_decode(DecodeLaunch& a) {
 hipError_t launch_decode(const DecodeLaunch& a, hipStream_t stream) {
   const void* f = a.bf16 ? (a.e4m3 ? (const void*)decode_kernel<true, true> : (const void*)decode_kernel<true, false>)
                          : (a.e4m3 ? (const void*)decode_kernel<false, true> : (const void*)decode_kernel<false, false>);
-  const hipError_t e =
-      launch_one(f, dim3(a.nsplit, a.c.num_kv_heads, a.b.n_seqs), kDecodeThreads, stream, a);
+  const hipError_t e = launch_one(f, dim3(a.nsplit, a.c.num_kv_heads, a.b.n_seqs), NW * kWave, stream, a);
   if (e != hipSuccess || a.nsplit == 1) return e;
   return launch_one(a.bf16 ? (const void*)merge_parts_kernel<true> : (const void*)merge_parts_kernel<false>,
-                    dim3(a.group, a.c.num_kv_heads, a.b.n_seqs), 256, stream, a);
+                    dim3(4 * a.group, a.c.num_kv_heads, a.b.n_seqs), 256, stream, a);
 }
 
 }  // namespace prr
