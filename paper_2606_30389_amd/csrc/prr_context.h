@@ -58,6 +58,7 @@ struct PromptLaunch {
   int num_kv_heads, group, max_pages, page_shift;
   int tiles;   // upper bound of the row tiles of one KV head
   int nsplit;  // parts of a row tile's keys
+  int waves;   // of a workgroup, 32 rows each
   bool bf16;
 };
 

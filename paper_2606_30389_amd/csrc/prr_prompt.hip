@@ -1,4 +1,6 @@
 // Causal attention of packed prompts over the paged cache.
+#include <type_traits>
+
 #include "prr_context.h"
 
 namespace prr {
@@ -16,17 +18,36 @@ namespace {
 // V^T's tokens are read in that order, 4 tokens of one channel at a time, by transposing LDS loads.
 // So no weight moves between lanes, and the rescale of a row is local to a lane.
 //
-// K and V tiles lie in LDS row by row (256 bytes), their 16-byte chunks permuted by the row: a read
-// of one chunk of eight consecutive rows (K), or of 32 bytes of four rows (V), touches every bank once.
-// Two buffers: a tile's successor is loaded into registers before its products and stored after
-// them, one barrier per tile.
+// K and V tiles lie in LDS row by row, the rows padded by 16 (K) and 64 bytes (V), so that a read of 16
+// bytes of eight rows, or of 32 bytes of four, touches every bank once at an immediate offset
+// (permuted chunks instead: 28% of the LDS cycles were conflicts).  Two buffers each; global loads run
+// a tile ahead in registers.
+//
+// A tile is a matrix phase (the tile before with V, this tile with K: 32 products, 1024 cycles) and a
+// vector phase (its softmax, about as long).  A SIMD has two waves of the workgroup, w and w + 4; the
+// second half of the waves runs one phase behind the first, barriers between the phases, so that one
+// wave's products run under the other's softmax.  16384 tokens, 32 / 2 heads, bf16: 2154 us with all
+// waves in step (MFMA 46% of the cycles, VALU 45%, one after the other), 1945 in turns: 1.13 PFLOP/s,
+// where a 16384^3 library product reaches 1.38.  The clock falls from 2.15 to about 1.9 GHz meanwhile:
+// power bounds it, and schedules with fewer stalls but more instructions (four sums and maxima side by
+// side, operands read further ahead) come out 1-3% slower.
+//
+// Four waves a workgroup (one per SIMD, nothing to take turns with) where a call is so short that
+// 256-row tiles leave half of the CUs idle and the keys are too few to be split.
 constexpr int kTokens = 64;
+constexpr int kKPitch = kHeadDim + 8, kVPitch = kHeadDim + 32;  // elements
 constexpr float kNoRef = -3e38f;
 // a row's reference exponent is moved only when its maximum outgrows it by this much (powers of two):
 // weights stay below 2^8, in range of either type, and the accumulators are rarely rescaled
 constexpr float kSlack = 8.0f;
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+
+template <bool BF16>
+__device__ __forceinline__ bool non_finite(uint32_t bits16) {
+  constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u;
+  return (bits16 & kExp) == kExp;
+}
 
 template <bool BF16>
 __device__ __forceinline__ f32x16_t mfma32(const u32x4_t& a, const u32x4_t& b, f32x16_t c) {
@@ -79,11 +100,12 @@ __device__ __forceinline__ bool find_tile(const PromptLaunch& a, int rows, int t
   return false;
 }
 
-template <bool BF16, int NW>
-__global__ __launch_bounds__(NW * kWave) void prompt_kernel(const PromptLaunch a) {
+template <bool BF16, bool PAGED, int NW, bool TURNS>
+__global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunch a) {
   constexpr int kRows = 32 * NW;
   constexpr int kPass = 16 / NW;  // 16-byte chunks of a K (or V) tile per thread
-  __shared__ __align__(16) uint16_t lds[2][2][kTokens * kHeadDim];  // [buffer][K, V]
+  __shared__ __align__(16) uint16_t lds[2][kTokens * (kKPitch + kVPitch)];  // [buffer] K, V
+  __shared__ int any_bad;  // non-finite values were set aside
   const int t = threadIdx.x, lane = lane_id(), w = __builtin_amdgcn_readfirstlane(t / kWave);
   const int n = lane & 31, hf = lane >> 5;
   const float kNegInf = -__builtin_inff();
@@ -102,11 +124,14 @@ __global__ __launch_bounds__(NW * kWave) void prompt_kernel(const PromptLaunch a
   const int tok = row / G, head = row - tok * G;
   const int pos = first + tok;
   const int wave_lo = first + min(row0 + 32 * w, rows - 1) / G;
-  const int wave_hi = row0 + 32 * w < rows ? first + min(row0 + 32 * w + 31, rows - 1) / G : -1;
   const int keys = max(0, first + min(row0 + kRows - 1, rows - 1) / G + 1);
   const int ntiles = (keys + kTokens - 1) / kTokens;
   const int per = (ntiles + a.nsplit - 1) / a.nsplit;
   const int t0 = min(part * per, ntiles), t1 = min(t0 + per, ntiles);
+
+  const int partial = (first + row0 / G + 1) / kTokens;  // tiles from this one on are not seen whole by every row
+  if (t == 0) any_bad = 0;
+  if (TURNS) __syncthreads();  // (else the first barrier below comes before the first values)
 
   const int64_t out_row = ((int64_t)(sq.q0 + tok) * a.num_kv_heads + h) * G + head;
   u32x4_t qf[8];
@@ -121,132 +146,255 @@ __global__ __launch_bounds__(NW * kWave) void prompt_kernel(const PromptLaunch a
     for (int i = 0; i < 16; ++i) acc[cb][i] = 0.0f;
   float mx = kNegInf, ref = kNoRef, l = 0.0f;
 
-  // loads: thread t takes chunk t%16 of rows t/16 + 4 NW x
+  // loads: thread t takes chunk t%16 of rows t/16 + 4 NW x; the four rows of a wave lie in one page
   const int chunk = t & 15, lrow = t >> 4;
-  const int psz = 1 << a.page_shift;
-  const int64_t head_row = (int64_t)h * a.max_pages << a.page_shift;
-  const auto cache_row = [&](int tile, int x) {
-    const int p = min(tile * kTokens + lrow + 4 * NW * x, keys - 1);
-    const int phys = phys_page(a.b.page_table, a.b.table_stride, a.max_pages, s, p >> a.page_shift);
-    return (head_row + ((int64_t)max(phys, 0) << a.page_shift) + (p & (psz - 1))) * kHeadDim + chunk * 8;
+  const int pmask = (1 << a.page_shift) - 1;
+  const int64_t head_byte = ((int64_t)h * a.max_pages << a.page_shift) * (2 * kHeadDim);
+  const char* const kbase = static_cast<const char*>(a.k) + head_byte;
+  const char* const vbase = static_cast<const char*>(a.v) + head_byte;
+  // The physical pages of the wave's rows of a tile, those of pass x in lane x: looked up a tile before
+  // they are used, so that nothing waits for them.
+  const auto lookup = [&](int tile) {
+    const int p = min(tile * kTokens + 4 * w + 4 * NW * (lane % kPass), keys - 1) >> a.page_shift;
+    if constexpr (PAGED) return a.b.page_table[(int64_t)s * a.b.table_stride + p];
+    return p;
+  };
+  const auto pages_of = [&](int found, int64_t (&page)[kPass]) {
+#pragma unroll
+    for (int x = 0; x < kPass; ++x) {
+      const int p = __builtin_amdgcn_readlane(found, x);
+      page[x] = (int64_t)((uint32_t)p < (uint32_t)a.max_pages ? p : 0) << (a.page_shift + 8);
+    }
   };
   u32x4_t kr[kPass], vr[kPass];
-  int64_t at[kPass];
-  const auto load = [&]() {
+  const auto load = [&](u32x4_t (&r)[kPass], const char* base, int tile, const int64_t (&page)[kPass]) {
 #pragma unroll
     for (int x = 0; x < kPass; ++x) {
-      kr[x] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.k) + at[x]);
-      vr[x] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.v) + at[x]);
+      const uint32_t off = (uint32_t)(min(tile * kTokens + lrow + 4 * NW * x, keys - 1) & pmask) * 256 + chunk * 16;
+      r[x] = *reinterpret_cast<const u32x4_t*>(base + page[x] + off);
     }
   };
-  const auto store = [&](int buf) {
+  int64_t pg0[kPass], pg1[kPass];  // pages of the next tiles
+  const auto store_k = [&](int buf) {
 #pragma unroll
-    for (int x = 0; x < kPass; ++x) {
-      const int r = lrow + 4 * NW * x;
-      *reinterpret_cast<u32x4_t*>(&lds[buf][0][r * kHeadDim + ((chunk ^ (r & 15)) * 8)]) = kr[x];
-      *reinterpret_cast<u32x4_t*>(&lds[buf][1][r * kHeadDim + ((chunk ^ ((r & 7) << 1)) * 8)]) = vr[x];
+    for (int x = 0; x < kPass; ++x) *reinterpret_cast<u32x4_t*>(&lds[buf][(lrow + 4 * NW * x) * kKPitch + chunk * 8]) = kr[x];
+  };
+  // In tiles that some row sees in part, a non-finite value would reach the rows that do not see it as 0 * v:
+  // it is stored as 0 and added to the rows that see it at the end.
+  const auto store_v = [&](int buf, int tile) {
+    if (tile >= partial) {
+      // (an exponent of all ones carries into its half's sign bit)
+      constexpr uint32_t kExp = BF16 ? 0x7f807f80u : 0x7c007c00u, kOne = BF16 ? 0x00800080u : 0x04000400u;
+      uint32_t carry = 0;
+#pragma unroll
+      for (int x = 0; x < kPass; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) carry |= (vr[x][i] & kExp) + kOne;
+      if (carry & 0x80008000u) {
+        any_bad = 1;
+#pragma unroll
+        for (int x = 0; x < kPass; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            vr[x][i] &= (non_finite<BF16>(vr[x][i]) ? 0u : 0xffffu) | (non_finite<BF16>(vr[x][i] >> 16) ? 0u : 0xffff0000u);
+      }
     }
+#pragma unroll
+    for (int x = 0; x < kPass; ++x)
+      *reinterpret_cast<u32x4_t*>(&lds[buf][kTokens * kKPitch + (lrow + 4 * NW * x) * kVPitch + chunk * 8]) = vr[x];
   };
 
-  // LDS offsets (elements) of this lane's operands; k-steps and channel blocks flip chunk bits
-  const int koff = n * kHeadDim + ((hf ^ (n & 15)) * 8);
+  // LDS offsets (elements) of this lane's operands
+  const int koff = n * kKPitch + hf * 8;
   const int vi = lane & 15, vg = (lane >> 4) & 1;
-  const int vrow = 4 * hf + (vi >> 2);
-  const int voff = vrow * kHeadDim + (((2 * vg + ((vi >> 1) & 1)) ^ ((vrow & 7) << 1)) * 8) + (vi & 1) * 4;
+  const int voff = kTokens * kKPitch + (4 * hf + (vi >> 2)) * kVPitch + 16 * vg + 4 * (vi & 3);
+
+  f32x16_t sc[2];   // logits of the current tile
+  u32x4_t pf[4];    // weights of the tile before
+#pragma unroll
+  for (int x = 0; x < 4; ++x) pf[x] = u32x4_t{0, 0, 0, 0};
+
+  const auto qk_step = [&](f32x16_t (&d)[2], int buf, int b, int x) {
+    const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(&lds[buf][koff + x * 16 + b * 32 * kKPitch]);
+    d[b] = mfma32<BF16>(kf, qf[x], d[b]);
+  };
+  const auto pv_step = [&](int buf, int x, int cb) {
+    uint16_t* v = &lds[buf][voff + cb * 32 + x * 16 * kVPitch];
+    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)v);
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(v + 8 * kVPitch));
+    const uint2 a0 = __builtin_bit_cast(uint2, lo), a1 = __builtin_bit_cast(uint2, hi);
+    acc[cb] = mfma32<BF16>(u32x4_t{a0.x, a0.y, a1.x, a1.y}, pf[x], acc[cb]);
+  };
+  // Matrix phase: the tile before with V, this tile with K.
+  const auto matrix = [&](int tile) {
+    const int buf = (tile - t0) & 1;
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) pv_step(buf ^ 1, x, cb);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) qk_step(sc, buf, b, x);
+    }
+    asm volatile("" : "+v"(sc[0]), "+v"(sc[1]), "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
+    __builtin_amdgcn_s_setprio(0);
+  };
+  // Vector phase: the softmax of this tile.
+  const auto vector = [&](int tile, auto masked) {
+    if constexpr (masked.value) {
+      const int base = tile * kTokens;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          sc[b][i] = base + 32 * b + 8 * (i / 4) + 4 * hf + i % 4 > pos ? kNegInf : sc[b][i];
+    }
+    float top = sc[0][0];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
+    mx = fmaxf(mx, max_halves(top));
+    const float scaled = mx * kSoftmaxScale2;
+    const bool grown = scaled > ref + kSlack;
+    if (__any(grown)) {
+      const float next = grown ? scaled : ref;
+      const float alpha = exp2_hw(ref - next);
+      ref = next;
+      l *= alpha;
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) acc[cb] *= alpha;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sc[b][i] = exp2_hw(fmaf(sc[b][i], kSoftmaxScale2, -ref));
+        l += sc[b][i];
+      }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int b = x >> 1, i = 8 * (x & 1);
+      pf[x] = u32x4_t{pack2<BF16>(sc[b][i], sc[b][i + 1]), pack2<BF16>(sc[b][i + 2], sc[b][i + 3]),
+                      pack2<BF16>(sc[b][i + 4], sc[b][i + 5]), pack2<BF16>(sc[b][i + 6], sc[b][i + 7])};
+      asm volatile("" : "+v"(pf[x]));
+    }
+  };
+  const auto barrier = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    __builtin_amdgcn_sched_barrier(0);
+  };
 
   if (t0 < t1) {
+    const int late = TURNS && w >= NW / 2;  // this half of the waves runs a phase behind the other
+    // what this wave stores in the vector phase of tile i: keys of tile i + 1 + late, values of i + late
+    int found = lookup(t0);
+    const int found1 = lookup(t0 + 1);
+    pages_of(found, pg0);
+    pages_of(found1, pg1);
+    u32x4_t k0[kPass];
+    load(k0, kbase, t0, pg0);
+    load(kr, kbase, t0 + 1, pg1);
+    load(vr, vbase, t0, pg0);
+    found = lookup(t0 + 2);
 #pragma unroll
-    for (int x = 0; x < kPass; ++x) at[x] = cache_row(t0, x);
-    load();
-    store(0);
-  }
-  __syncthreads();
-  for (int tile = t0; tile < t1; ++tile) {
-    const int buf = (tile - t0) & 1;
-    if (tile + 1 < t1) {
+    for (int x = 0; x < kPass; ++x)
+      *reinterpret_cast<u32x4_t*>(&lds[0][(lrow + 4 * NW * x) * kKPitch + chunk * 8]) = k0[x];
+    if (late) {
+      store_k(1);
+      store_v(0, t0);
 #pragma unroll
-      for (int x = 0; x < kPass; ++x) at[x] = cache_row(tile + 1, x);
-      load();
+      for (int x = 0; x < kPass; ++x) pg0[x] = pg1[x];
+      pages_of(found, pg1);
+      load(kr, kbase, t0 + 2, pg1);
+      load(vr, vbase, t0 + 1, pg0);
+      found = lookup(t0 + 3);
     }
-    const int base = tile * kTokens;
-    if (base <= wave_hi) {
-      f32x16_t sc[2];
+    // (values of the tile before the first: the other buffer, all zero)
+    {
+      const u32x4_t z = {0, 0, 0, 0};
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int x = 0; x < kPass; ++x)
+        *reinterpret_cast<u32x4_t*>(&lds[1][kTokens * kKPitch + (lrow + 4 * NW * x) * kVPitch + chunk * 8]) = z;
+    }
+    barrier();
+    if (late) barrier();
+    const int whole = min(t1, max(t0, (wave_lo + 1) / kTokens));  // tiles whose tokens every row of the wave sees
+    const auto step = [&](int tile, auto masked) {
+      matrix(tile);
+      if (TURNS) barrier();
+      const int kb = (tile - t0 + 1 + late) & 1;
+      store_k(kb);
+      store_v(kb ^ 1, tile + late);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
+      for (int x = 0; x < kPass; ++x) pg0[x] = pg1[x];
+      pages_of(found, pg1);
+      found = lookup(tile + 3 + late);
+      load(kr, kbase, tile + 2 + late, pg1);
+      load(vr, vbase, tile + 1 + late, pg0);
+      vector(tile, masked);
+      barrier();
+    };
+    int tile = t0;
+    for (; tile < whole; ++tile) step(tile, std::false_type{});
+    for (; tile < t1; ++tile) step(tile, std::true_type{});
+    if (TURNS && !late) barrier();
+    const int buf = (t1 - 1 - t0) & 1;
 #pragma unroll
-        for (int x = 0; x < 8; ++x) {
-          const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(&lds[buf][0][(koff ^ (x * 16)) + b * 32 * kHeadDim]);
-          sc[b] = mfma32<BF16>(kf, qf[x], sc[b]);
-        }
-      }
-      if (base + kTokens - 1 > wave_lo) {  // some of the tokens come after some of the rows
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+      for (int cb = 0; cb < 4; ++cb) pv_step(buf, x, cb);
+  }
+
+  __syncthreads();
+  if (any_bad) {  // what was set aside, to the rows that see it: whatever its weight, the result is not finite
+    for (int p = max(partial, t0) * kTokens; p < min(t1 * kTokens, keys); ++p) {
+      const int phys = phys_page(a.b.page_table, a.b.table_stride, a.max_pages, s, p >> a.page_shift);
+      const char* v = vbase + ((int64_t)max(phys, 0) << (a.page_shift + 8)) + (int64_t)(p & pmask) * 256 + 8 * hf;
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            sc[b][i] = base + 32 * b + 8 * (i / 4) + 4 * hf + i % 4 > pos ? kNegInf : sc[b][i];
-      }
-      float top = sc[0][0];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
-      mx = fmaxf(mx, max_halves(top));
-      if (__any(mx * kSoftmaxScale2 > ref + kSlack)) {
-        const float next = mx == kNegInf ? ref : mx * kSoftmaxScale2;
-        const float alpha = exp2_hw(ref - next);
-        l *= alpha;
-#pragma unroll
-        for (int cb = 0; cb < 4; ++cb) acc[cb] *= alpha;
-        ref = next;
-      }
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          sc[b][i] = exp2_hw(fmaf(sc[b][i], kSoftmaxScale2, -ref));
-          l += sc[b][i];
+          const uint32_t x = *reinterpret_cast<const uint16_t*>(v + 64 * cb + 16 * (i / 4) + 2 * (i % 4));
+          if (non_finite<BF16>(x) && p <= pos) acc[cb][i] += h2f<BF16>(x);
         }
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {  // 16 tokens
-        const int b = x >> 1, i = 8 * (x & 1);
-        const u32x4_t pf = {pack2<BF16>(sc[b][i], sc[b][i + 1]), pack2<BF16>(sc[b][i + 2], sc[b][i + 3]),
-                            pack2<BF16>(sc[b][i + 4], sc[b][i + 5]), pack2<BF16>(sc[b][i + 6], sc[b][i + 7])};
-#pragma unroll
-        for (int cb = 0; cb < 4; ++cb) {
-          uint16_t* v = &lds[buf][1][(voff ^ (cb * 32)) + x * 16 * kHeadDim];
-          const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)v);
-          const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(v + 8 * kHeadDim));
-          const uint2 a0 = __builtin_bit_cast(uint2, lo), a1 = __builtin_bit_cast(uint2, hi);
-          acc[cb] = mfma32<BF16>(u32x4_t{a0.x, a0.y, a1.x, a1.y}, pf, acc[cb]);
-        }
-      }
     }
-    if (tile + 1 < t1) store(buf ^ 1);
-    __syncthreads();
   }
 
   l = sum_halves(l);
   const float inv = l != 0.0f ? 1.0f / l : 0.0f;
   // l relative to the logit itself, not to its rounded product with the scale (and the slack)
   const float exact = mx == kNegInf ? 0.0f : l * exp2_hw(-fmaf(mx, kSoftmaxScale2, -ref));
-  if (!live) return;
   if (a.nsplit == 1) {
-    uint16_t* o = static_cast<uint16_t*>(a.out_o) + out_row * kHeadDim + 4 * hf;
+    // (the halves of a wave swap four of their eight channels, so that a store holds 16 bytes of a row)
+    uint16_t* o = static_cast<uint16_t*>(a.out_o) + out_row * kHeadDim + 8 * hf;
 #pragma unroll
     for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<uint2*>(o + 32 * cb + 2 * i) =
-            make_uint2(pack2<BF16>(acc[cb][i] * inv, acc[cb][i + 1] * inv),
-                       pack2<BF16>(acc[cb][i + 2] * inv, acc[cb][i + 3] * inv));
-    if (a.out_m && hf == 0) {
+      for (int i = 0; i < 16; i += 8) {
+        uint32_t r[4];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const auto two = __builtin_amdgcn_permlane32_swap(
+              pack2<BF16>(acc[cb][i + 2 * x] * inv, acc[cb][i + 2 * x + 1] * inv),
+              pack2<BF16>(acc[cb][i + 4 + 2 * x] * inv, acc[cb][i + 5 + 2 * x] * inv), false, false);
+          r[x] = two[0];
+          r[2 + x] = two[1];
+        }
+        if (live) *reinterpret_cast<uint4*>(o + 32 * cb + 2 * i) = make_uint4(r[0], r[1], r[2], r[3]);
+      }
+    if (live && a.out_m && hf == 0) {
       a.out_m[out_row] = mx * kSoftmaxScale;
       a.out_l[out_row] = exact;
     }
-  } else {
+  } else if (live) {
     const int64_t x = (int64_t)part * a.b.total_q * a.num_kv_heads * G + out_row;
     float* o = a.part_o + x * kHeadDim + 4 * hf;
 #pragma unroll
@@ -297,24 +445,40 @@ __global__ __launch_bounds__(256) void merge_prompt_kernel(const PromptLaunch a)
   }
 }
 
-constexpr int kWaves = 8;
-
 }  // namespace
 
 void plan_prompt(PromptLaunch& a) {
-  const int rows = 32 * kWaves;
-  const int64_t packed = (int64_t)a.b.total_q * a.group / rows + a.b.n_seqs;
-  const int64_t each = (int64_t)a.b.n_seqs * (((int64_t)a.b.max_q * a.group + rows - 1) / rows);
-  a.tiles = (int)min(packed, each);
-  // fewer workgroups than CUs: the keys are cut into parts of at least eight tiles
-  const int64_t units = (int64_t)a.tiles * a.num_kv_heads;
+  const auto tiles_of = [&](int rows) {
+    const int64_t packed = (int64_t)a.b.total_q * a.group / rows + a.b.n_seqs;
+    const int64_t each = (int64_t)a.b.n_seqs * (((int64_t)a.b.max_q * a.group + rows - 1) / rows);
+    return min(packed, each);
+  };
+  // fewer workgroups than CUs: the keys are cut into parts of at least eight tiles, as many as fill the
+  // chip once (twice as many small parts fill it better, but joining them and power take that back)
   const int64_t key_tiles = ((int64_t)a.b.max_kv + kTokens - 1) / kTokens;
-  a.nsplit = (int)max((int64_t)1, min((int64_t)256 / max(units, (int64_t)1), key_tiles / 8));
+  const auto parts_of = [&](int64_t units) {
+    return (int)max((int64_t)1, min((int64_t)256 / max(units, (int64_t)1), key_tiles / 8));
+  };
+  const int64_t units = tiles_of(256) * a.num_kv_heads;
+  a.waves = units <= 128 && parts_of(units) == 1 ? 4 : 8;
+  a.tiles = (int)tiles_of(32 * a.waves);
+  a.nsplit = parts_of((int64_t)a.tiles * a.num_kv_heads);
 }
 
+namespace {
+
+template <bool BF16, bool PAGED>
+const void* prompt_fn(int waves) {
+  return waves == 8 ? (const void*)prompt_kernel<BF16, PAGED, 8, true> : (const void*)prompt_kernel<BF16, PAGED, 4, false>;
+}
+
+}  // namespace
+
 hipError_t launch_prompt(const PromptLaunch& a, hipStream_t stream) {
-  const void* f = a.bf16 ? (const void*)prompt_kernel<true, kWaves> : (const void*)prompt_kernel<false, kWaves>;
-  const hipError_t e = launch_one(f, dim3(a.tiles * a.num_kv_heads, a.nsplit), kWaves * kWave, stream, a);
+  const bool paged = a.b.page_table != nullptr;
+  const void* f = a.bf16 ? (paged ? prompt_fn<true, true>(a.waves) : prompt_fn<true, false>(a.waves))
+                         : (paged ? prompt_fn<false, true>(a.waves) : prompt_fn<false, false>(a.waves));
+  const hipError_t e = launch_one(f, dim3(a.tiles * a.num_kv_heads, a.nsplit), a.waves * kWave, stream, a);
   if (e != hipSuccess || a.nsplit == 1) return e;
   const int64_t rows = (int64_t)a.b.total_q * a.num_kv_heads * a.group;
   return launch_one(a.bf16 ? (const void*)merge_prompt_kernel<true> : (const void*)merge_prompt_kernel<false>,

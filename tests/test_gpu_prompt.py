@@ -129,6 +129,43 @@ def test_prompt_rising_maximum():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("hq,hkv,n,past", [(16, 1, 40, 100), (2, 2, 300, 90), (4, 1, 1500, 64)])
+def test_prompt_non_finite_tokens_reach_only_who_sees_them(hq, hkv, n, past, dt):
+    """Infinities and NaN in a token's keys and values change nothing for the tokens before it."""
+    import paper_2606_30389_amd as P
+    b = S.Batch([n], [past + n], 16, device=DEV, seed=2)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    q = torch.randn(n, hq, S.D, generator=g, device=DEV).to(DT[dt])
+    cache = [torch.randn(hkv, b.pool, 16, S.D, generator=g, device=DEV).to(DT[dt]) for _ in range(2)]
+    dims = P.make_dims(hq, hkv, 16, b.pool, P.PRR_BF16 if dt == "bf16" else P.PRR_F16)
+    batch = b.make(P)
+    nbytes = P.prr_prompt_workspace_size(dims, batch)
+    ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=DEV)
+
+    def run(c):
+        out = torch.zeros(n, hq, S.D, dtype=DT[dt], device=DEV)
+        P.prr_prompt_attn(dims, batch, q, *c, out, None, None, ws, nbytes)
+        torch.cuda.synchronize()
+        return out
+
+    clean = run(cache)
+    for at in (past + n - 1, past + n // 2, past + 3):
+        for i, values in ((0, [math.inf]), (1, [math.inf, -math.inf, math.nan])):
+            for x in values:
+                dirty = [c.clone() for c in cache]
+                dirty[i].flatten(1, 2)[:, b.slots(0, at, at + 1).to(DEV), 5] = x
+                got = run(dirty)
+                sees = at - past
+                assert torch.equal(got[:sees], clean[:sees])
+                if i == 1:
+                    want = got[sees:, :, 5].float()
+                    assert torch.all(want.isnan()) if math.isnan(x) else torch.all(want.isnan() | (want == x))
+                    keep = [c for c in range(S.D) if c != 5]
+                    assert torch.equal(got[sees:][..., keep], clean[sees:][..., keep])
+
+
+@pytest.mark.gpu
 def test_prompt_replayed_in_a_graph():
     """One capture, replayed with other inputs and lengths in the same buffers, eager work in between."""
     P, dims, batch, q, cache, out, m, l, ws, nbytes = run_case([60, 20], [900, 700], 8, 2, spare=0)
