@@ -312,15 +312,20 @@ def make_batch(n_seqs, total_q, max_q, max_kv, cu_q, kv_len, page_table=None, ta
     return b
 
 
+_torch = None
+
+
 def _on_device(fn, like, stream, *args):
     """fn(*args, stream) with `like`'s device current; stream None = that device's current stream."""
-    device = getattr(like, "device", None)
-    if device is None or device.type != "cuda":
+    global _torch
+    if not getattr(like, "is_cuda", False):
         return _check(fn(*args, _stream(stream)))
-    import torch
-    if device.index == torch.cuda.current_device():
-        return _check(fn(*args, torch._C._cuda_getCurrentRawStream(device.index) if stream is None else _stream(stream)))
-    with torch.cuda.device(device):
+    if _torch is None:
+        import torch as _torch
+    index = like.get_device()
+    if index == _torch._C._cuda_getDevice():
+        return _check(fn(*args, _torch._C._cuda_getCurrentRawStream(index) if stream is None else _stream(stream)))
+    with _torch.cuda.device(index):
         return _check(fn(*args, _stream(stream)))
 
 
@@ -328,10 +333,10 @@ def _row_stride(x, heads, name):
     """Elements between rows of x [rows][heads][128] (a tensor dense within a row), or of a dense array."""
     if x is None or isinstance(x, int):
         return heads * 128
-    if x.dim() != 3 or x.shape[1:] != (heads, 128) or x.stride()[1:] != (128, 1):
-        raise ValueError(f"{name} has shape {tuple(x.shape)}, strides {x.stride()}: expected [rows][{heads}][128], "
-                         "dense within a row")
-    return x.stride(0)
+    shape, stride = x.shape, x.stride()
+    if len(shape) == 3 and shape[1] == heads and shape[2] == 128 and stride[2] == 1 and (stride[1] == 128 or heads == 1):
+        return stride[0]
+    raise ValueError(f"{name} has shape {tuple(shape)}, strides {stride}: expected [rows][{heads}][128], dense within a row")
 
 
 def prr_rope_freqs(kind, rot_dim, base, factor=1.0, trained_len=1, lo=1.0, hi=32.0):

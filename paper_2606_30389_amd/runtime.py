@@ -10,10 +10,14 @@ the selection is in flight; repair waits for both; the EMA update and the next
 prediction wait for the selection only and are off the critical path.  The serial
 baseline is score_topk followed by repair with no prediction, on one stream.
 
+Around the step, PagedCache (and a LayerState's prefill and append) writes new tokens with their rotary
+positions into the paged cache, attends prompts and whole caches, and keeps a cache in e4m3.
+
 All arithmetic happens in libprr.so; this module only allocates, uploads and orders.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
 from typing import List, Optional, Sequence
@@ -73,6 +77,130 @@ def bits_tensor(bits: np.ndarray, dtype: torch.dtype, device) -> torch.Tensor:
     return t.to(device).view(dtype)
 
 
+class Rope:
+    """Rotary positions of a model: frequencies (prr_rope_freqs, or given) on the device, layout and scale."""
+
+    KINDS = {"plain": L.PRR_ROPE_PLAIN, "linear": L.PRR_ROPE_LINEAR, "ntk": L.PRR_ROPE_NTK,
+             "by_parts": L.PRR_ROPE_BY_PARTS, "yarn": L.PRR_ROPE_YARN}
+
+    def __init__(self, device, rot_dim=128, base=10000.0, kind="plain", factor=1.0, trained_len=1, lo=1.0, hi=32.0,
+                 interleaved=False, freqs=None, scale=1.0):
+        if freqs is None:
+            freqs, scale = L.prr_rope_freqs(self.KINDS[kind], rot_dim, base, factor, trained_len, lo, hi)
+        self.freqs = torch.as_tensor(freqs, dtype=torch.float64).to(device)
+        self.rot_dim, self.scale = 2 * self.freqs.numel(), float(scale)
+        self.layout = L.PRR_ROPE_INTERLEAVED if interleaved else L.PRR_ROPE_HALF
+
+
+class Batch:
+    """The sequences of a call: their new tokens, their tokens in the cache (the new ones included) and
+    their rows of the page table.  The lengths live on the device (cu_q, kv_len), where a captured graph
+    reads them; max_q and max_kv bound them for as long as the batch is used."""
+
+    def __init__(self, device, new: Sequence[int], kv: Sequence[int], page_table=None, max_q=None, max_kv=None, total_q=None):
+        cu = np.concatenate([[0], np.cumsum(np.asarray(new, dtype=np.int64))]).astype(np.int32)
+        self.kv_len = torch.tensor(list(kv), dtype=torch.int32, device=device)
+        self.page_table = page_table
+        # one new token each: rows are sequences
+        self.cu_q = None if all(n == 1 for n in new) else torch.from_numpy(cu).to(device)
+        self.total_q = int(cu[-1]) if total_q is None else total_q
+        self.native = L.make_batch(len(self.kv_len), self.total_q, max(new) if max_q is None else max_q,
+                                   max(kv) if max_kv is None else max_kv, self.cu_q, self.kv_len, page_table,
+                                   0 if page_table is None else page_table.shape[-1])
+
+    def advance(self):
+        """Every sequence is one token longer (on the current stream)."""
+        self.kv_len.add_(1)
+
+
+def _stream_context(stream):
+    """What is allocated inside belongs to `stream` (None: the current one), as the kernels that write it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+
+
+class PagedCache:
+    """One layer's paged cache, in 16 bits or e4m3, for any number of sequences: new tokens are appended with
+    their rotary positions, prompts and single tokens attend it, e4m3 pages are read back.
+
+    Each stream has workspaces of its own, kept for as long as the cache: a captured graph may hold any of
+    them.  Outputs that are not given are allocated on the call's stream."""
+
+    def __init__(self, cfg: PathConfig, device, kind="16", k=None, v=None):
+        self.cfg, self.dims = cfg, cfg.dims()
+        self.kind = {"16": L.PRR_KV_16, "e4m3": L.PRR_KV_E4M3}[kind]
+        shape = (cfg.num_kv_heads, self.dims.max_pages, cfg.page_size, 128)
+        dtype = cfg.torch_dtype if kind == "16" else torch.float8_e4m3fn
+        self.k = torch.zeros(shape, dtype=torch.uint8, device=device).view(dtype) if k is None and kind == "e4m3" else \
+            torch.zeros(shape, dtype=dtype, device=device) if k is None else k
+        self.v = torch.zeros_like(self.k) if v is None else v
+        self.k_scale = self.v_scale = None
+        if kind == "e4m3":  # (exponent bytes of the rows' powers of two: 127 is 1)
+            self.k_scale = torch.full(shape[:3], 127, dtype=torch.uint8, device=device)
+            self.v_scale = torch.full(shape[:3], 127, dtype=torch.uint8, device=device)
+        self._ws = {}
+
+    def _workspace(self, nbytes, stream):
+        if not nbytes:
+            return None
+        kept = self._ws.setdefault(L._stream(stream), [])
+        if not kept or kept[-1].numel() < nbytes:
+            kept.append(torch.empty(nbytes, dtype=torch.uint8, device=self.k.device))
+        return kept[-1]
+
+    def append(self, batch: Batch, q, k, v, rope: Optional[Rope] = None, positions=None, q_out=None, stream=None):
+        """New tokens' keys and values into the cache, rotated; returns the rotated queries."""
+        if q is not None and q_out is None:
+            with _stream_context(stream):
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        L.prr_rope_append(self.dims, batch.native, q, k, v, positions, None if rope is None else rope.freqs,
+                          0 if rope is None else rope.rot_dim, L.PRR_ROPE_HALF if rope is None else rope.layout,
+                          1.0 if rope is None else rope.scale, q_out, self.kind, self.k, self.v, self.k_scale, self.v_scale,
+                          stream)
+        return q_out
+
+    def prompt(self, batch: Batch, q, out=None, stream=None):
+        """Causal attention of the new tokens: (o in the 16-bit type, m, l)."""
+        if self.kind != L.PRR_KV_16:
+            raise ValueError("prompts attend a 16-bit cache: read() the pages back first")
+        nbytes = L.prr_prompt_workspace_size(self.dims, batch.native)
+        with _stream_context(stream):
+            if out is None:
+                n, hq = q.shape[:2]
+                out = (torch.zeros_like(q), *(torch.zeros(n, hq, dtype=torch.float32, device=q.device) for _ in range(2)))
+            ws = self._workspace(nbytes, stream)
+        L.prr_prompt_attn(self.dims, batch.native, q, self.k, self.v, *out, ws, nbytes, stream)
+        return out
+
+    def attend(self, batch: Batch, q, pages=None, counts=None, out=None, stream=None):
+        """Attention of one token per sequence over its whole cache, or over listed pages
+        ([sequence][KV head][cap] and [sequence][KV head]): (o float32, o in the 16-bit type, m, l)."""
+        cap = 0 if pages is None else pages.shape[-1]
+        nbytes = L.prr_decode_workspace_size(self.dims, batch.native, self.kind, cap)
+        with _stream_context(stream):
+            if out is None:
+                n, hq = q.shape[:2]
+                f32 = dict(dtype=torch.float32, device=q.device)
+                out = (torch.zeros(n, hq, 128, **f32), torch.zeros_like(q), torch.zeros(n, hq, **f32), torch.zeros(n, hq, **f32))
+            ws = self._workspace(nbytes, stream)
+        L.prr_decode_attn(self.dims, batch.native, q, self.kind, self.k, self.v, self.k_scale, self.v_scale, pages, counts, cap,
+                          *out, ws, nbytes, stream)
+        return out
+
+    def read(self, num_tokens, page_table=None, page_begin=0, page_end=None, out=None, stream=None):
+        """Pages of a sequence of an e4m3 cache in 16 bits: (k, v) [Hkv][pages][page_size][128]."""
+        if page_end is None:
+            page_end = -(-num_tokens // self.cfg.page_size)
+        if out is None:
+            shape = (self.cfg.num_kv_heads, page_end - page_begin, self.cfg.page_size, 128)
+            with _stream_context(stream):
+                out = tuple(torch.zeros(shape, dtype=self.cfg.torch_dtype, device=self.k.device) for _ in range(2))
+        L.prr_cache_read(self.dims, self.k, self.v, self.k_scale, self.v_scale, page_table, num_tokens, page_begin, page_end,
+                         *out, stream)
+        return out
+
+
 class LayerState:
     """Device memory of one layer: KV cache, metadata, EMA state, lists, partials, outputs."""
 
@@ -117,6 +245,36 @@ class LayerState:
         L.prr_workspace_init(self.workspace, self.ws_bytes)
         self.cur = 0  # which predicted-list buffer holds P^t
         self.theta = None  # this layer's (alpha, beta, gamma), host float32 [3], or None (the step's)
+
+    # --------------------------------------------------------------- prompts and new tokens
+    def cache(self) -> PagedCache:
+        """This layer's keys and values as a PagedCache (the same memory)."""
+        if getattr(self, "_cache", None) is None:
+            self._cache = PagedCache(self.cfg, self.k.device, k=self.k, v=self.v)
+        return self._cache
+
+    def batch(self, new_tokens) -> Batch:
+        """The layer's sequence with `new_tokens` new ones at the end of its cfg.num_tokens."""
+        table = None if self.page_table is None else self.page_table.view(1, -1)
+        return Batch(self.k.device, [new_tokens], [self.cfg.num_tokens], table)
+
+    def prefill(self, q, k, v, rope: Optional[Rope] = None, batch: Optional[Batch] = None, stream=None):
+        """The last len(q) of the cfg.num_tokens tokens: into the cache, their causal attention, and the metadata
+        of the pages that they touch.  q [n][Hq][128], k, v [n][Hkv][128]; returns (o, m, l)."""
+        cfg = self.cfg
+        batch = self.batch(q.shape[0]) if batch is None else batch
+        q = self.cache().append(batch, q, k, v, rope, stream=stream)
+        out = self.cache().prompt(batch, q, stream=stream)
+        self.build_meta(stream, page_begin=(cfg.num_tokens - q.shape[0]) // cfg.page_size)
+        return out
+
+    def append(self, q, k, v, rope: Optional[Rope] = None, batch: Optional[Batch] = None, q_out=None, stream=None):
+        """One new token, the last of the cfg.num_tokens: into the cache, and its page's metadata; returns the
+        rotated query, ready for select() or a decode step."""
+        cfg = self.cfg
+        q = self.cache().append(self.batch(1) if batch is None else batch, q, k, v, rope, q_out=q_out, stream=stream)
+        self.build_meta(stream, page_begin=(cfg.num_tokens - 1) // cfg.page_size)
+        return q
 
     # --------------------------------------------------------------- steps
     def build_meta(self, stream=None, page_begin=0, page_end=None):
@@ -260,6 +418,12 @@ class DecodeStack:
         for i, st in enumerate(self.layers):
             st.theta = None if thetas is None else np.asarray(thetas[i], dtype=np.float32).copy()
             self.io[i].theta = None if st.theta is None else st.theta.ctypes.data
+
+    def set_tokens(self, num_tokens):
+        """The sequence now holds num_tokens tokens: for the next steps of every layer."""
+        for st in self.layers:
+            st.cfg.num_tokens = num_tokens
+        self.params.num_tokens, self.params.num_pages = self.cfg.num_tokens, self.cfg.num_pages
 
     def _parity(self):
         parity = self.layers[0].cur

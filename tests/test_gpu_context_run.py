@@ -1,0 +1,225 @@
+"""The calls around the decode step as a program uses them: a prompt into the cache, its attention, page metadata, then
+tokens by the decode step, over 16-bit and e4m3 caches, on one stream and in captured graphs; pools beyond 2^31
+elements."""
+import math
+
+import pytest
+import torch
+
+from tests import context_support as S
+
+DEV = "cuda:0"
+DT = {"bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def causal64(q, k, v, past):
+    """q [n][Hq][128], k, v [tokens][Hkv][128] in 64 bits: o, m, l, weights times |v|, the logits' magnitudes."""
+    n, hq = q.shape[:2]
+    hkv, G = k.shape[1], q.shape[1] // k.shape[1]
+    parts = []
+    vis = (torch.arange(k.shape[0], device=q.device) <= past + torch.arange(n, device=q.device)[:, None]).repeat_interleave(G, 0)
+    for h in range(hkv):
+        r = S.attend64(q[:, h * G:(h + 1) * G].reshape(-1, S.D), k[:, h], v[:, h], vis)
+        parts.append([x.view(n, G, *x.shape[1:]) for x in r])
+    return [torch.cat([p[i] for p in parts], 1).flatten(0, 1) for i in range(5)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt,hq,hkv,page,paged", [("bf16", 32, 2, 16, False), ("f16", 8, 2, 64, True)])
+def test_prompt_then_decode_steps(dt, hq, hkv, page, paged):
+    """300 prompt tokens, then 40 more one by one: the decode step with a budget of every page is dense attention, and so
+    is the whole-cache call."""
+    import paper_2606_30389_amd as P
+    from paper_2606_30389_amd import runtime as R
+    n0, steps = 300, 40
+    pages = -(-(n0 + steps) // page)
+    pc = R.PathConfig(num_q_heads=hq, num_kv_heads=hkv, page_size=page, num_tokens=n0, k_select=pages, dtype=dt,
+                      chunk_pages=max(1, 64 // page), max_pages=pages + 5)
+    pc_cap = R.PathConfig(**{**pc.__dict__, "num_tokens": n0 + steps})
+    table = torch.randperm(pages + 5, generator=torch.Generator().manual_seed(1))[:pages + 5].to(torch.int32).to(DEV) if paged else None
+    st = R.LayerState(pc_cap, DEV, page_table=table)  # (lists for the longest context)
+    st.cfg = pc
+    rope = R.Rope(DEV, rot_dim=64, base=10000.0, kind="yarn", factor=4.0, trained_len=128, interleaved=True)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    qkv = torch.randn(n0 + steps, hq + 2 * hkv, S.D, generator=g, device=DEV).to(DT[dt])
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    pos = torch.arange(n0 + steps)
+    # rotated once in 64 bits, rounded as the cache holds them
+    q64, k64 = (S.rotate64(x.cpu(), pos, rope.freqs.cpu(), 64, True, rope.scale)[0].to(DT[dt]).to(DEV) for x in (q, k))
+    o, m, l = st.prefill(q[:n0], k[:n0], v[:n0], rope)
+    torch.cuda.synchronize()
+    eps = S.half_step(DT[dt])
+    # (a rotated query or key may be rounded to the neighbour where 64 bits are next to a border: another half step)
+    slack = 2 * eps
+    want = causal64(q64[:n0].double(), k64[:n0].double(), v[:n0].double(), 0)
+    assert (o.double().flatten(0, 1) - want[0]).abs().max() <= 8 * eps * want[3].max()
+    assert ((m.double().flatten() - want[1]).abs() <= want[4] * slack + 1e-5).all()
+    cache = st.cache()
+    got = cache.k.flatten(1, 2).cpu()
+    slot = (table.cpu().long()[pos // page] if paged else pos // page) * page + pos % page
+    assert ((got[:, slot[:n0]].double() - k64[:n0].transpose(0, 1).double().cpu()).abs() <= slack * k64[:n0].transpose(0, 1).abs().double().cpu() + 1e-6).all()
+    qbuf = torch.empty(1, hq, S.D, dtype=DT[dt], device=DEV)
+    stack = R.DecodeStack([st], [qbuf], DEV)
+    one = R.Batch(DEV, [1], [n0], None if table is None else table.view(1, -1), max_kv=n0 + steps)
+    s = torch.cuda.current_stream()
+    for i in range(steps):
+        t = n0 + i
+        stack.set_tokens(t + 1)
+        one.advance()
+        st.append(q[t:t + 1], k[t:t + 1], v[t:t + 1], rope, batch=one, q_out=qbuf, stream=s)
+        stack.step(P.PRR_SCHED_FUSED_PREFILL if i == 0 else P.PRR_SCHED_FUSED_PRR, s)
+        if i == 0:  # (the first step selects and initialises the prediction; it attends nothing)
+            continue
+        dense = cache.attend(one, qbuf)
+        torch.cuda.synchronize()
+        w = causal64(qbuf.double(), k64[:t + 1].double(), v[:t + 1].double(), t)
+        for o32, mm, ll in ((st.out_o32, st.out_m, st.out_l), (dense[0][0], dense[2][0], dense[3][0])):
+            assert (o32.double() - w[0]).abs().max() <= 4 * eps * w[3].max()  # (keys a half step apart)
+        # the two calls attend the same keys: their states are the same but for float32
+        assert (st.out_o32 - dense[0][0]).abs().max() <= 2e-5 * (1 + dense[0].abs().max())
+        assert torch.allclose(st.out_m, dense[2][0], rtol=1e-5, atol=1e-5) and torch.allclose(st.out_l, dense[3][0], rtol=1e-4)
+
+
+@pytest.mark.gpu
+def test_quantised_batch_generates():
+    """Three sequences in an e4m3 pool: prompts appended, tokens appended and attended, pages read back for metadata, selection
+    and the 16-bit attention over the selected pages; the tokens' part replayed from a graph gives the same bits."""
+    import paper_2606_30389_amd as P
+    from paper_2606_30389_amd import runtime as R
+    page, hq, hkv, steps = 16, 16, 2, 6
+    lens = [100, 37, 250]
+    per = [-(-(n + steps) // page) for n in lens]
+    pool = sum(per) + 3
+    ids = torch.randperm(pool, generator=torch.Generator().manual_seed(0)).to(torch.int32)
+    table = torch.full((3, max(per)), -1, dtype=torch.int32)
+    at = 0
+    for i, p in enumerate(per):
+        table[i, :p] = ids[at:at + p]
+        at += p
+    pc = R.PathConfig(num_q_heads=hq, num_kv_heads=hkv, page_size=page, num_tokens=pool * page, k_select=4, max_pages=pool)
+    cache = R.PagedCache(pc, DEV, kind="e4m3")
+    rope = R.Rope(DEV, rot_dim=128, base=500000.0)
+    g = torch.Generator(device=DEV).manual_seed(7)
+    rand = lambda n: torch.randn(n, hq + 2 * hkv, S.D, generator=g, device=DEV).to(torch.bfloat16)  # noqa: E731
+    split = lambda x: (x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:])  # noqa: E731
+    d_table = table.to(DEV)
+    cache.append(R.Batch(DEV, lens, lens, d_table), *split(rand(sum(lens))), rope)
+    new = [rand(3) for _ in range(steps)]
+
+    def tokens(b, x):
+        qr = cache.append(b, *split(x), rope, q_out=bufs[0])
+        return qr, cache.attend(b, qr, out=bufs[1])
+
+    bufs = (torch.empty(3, hq, S.D, dtype=torch.bfloat16, device=DEV),
+            (torch.empty(3, hq, S.D, device=DEV), torch.empty(3, hq, S.D, dtype=torch.bfloat16, device=DEV),
+             torch.empty(3, hq, device=DEV), torch.empty(3, hq, device=DEV)))
+    b = R.Batch(DEV, [1] * 3, lens, d_table, max_kv=max(lens) + steps)
+    seen = []
+    for x in new:
+        b.advance()
+        qr, out = tokens(b, x)
+        torch.cuda.synchronize()
+        seen.append([t.clone() for t in (qr, *out)])
+        for s in range(3):
+            n = int(b.kv_len[s])
+            row = d_table[s].contiguous()
+            k16, v16 = cache.read(n, row)
+            for h in range(hkv):
+                kk, vv = (t[h].flatten(0, 1)[:n].double() for t in (k16, v16))
+                G = hq // hkv
+                o, m, l, a, mag = S.attend64(qr[s, h * G:(h + 1) * G].double(), kk, vv)
+                hs = slice(h * G, (h + 1) * G)
+                S.check_state(out[0][s, hs].double(), out[2][s, hs].double(), out[3][s, hs].double(), o, m, l, a, mag,
+                              2.0 ** -22, 2.0 ** -22, n, 2.0 ** -25 * n * float(vv.abs().max()))
+    # sequence 2's pages, read back: metadata, selection and the page-list attention of the 16-bit path, against the same
+    # pages of the e4m3 cache
+    n = int(b.kv_len[2])
+    k16, v16 = cache.read(n, d_table[2].contiguous())
+    pc2 = R.PathConfig(num_q_heads=hq, num_kv_heads=hkv, page_size=page, num_tokens=n, k_select=5)
+    st = R.LayerState(pc2, DEV, k=k16, v=v16)
+    st.build_meta()
+    qs = seen[-1][0][2]
+    st.select(qs)
+    st.repair(qs, serial=True)
+    listed = R.Batch(DEV, [1], [n], d_table[2:3])
+    out = cache.attend(listed, qs[None], st.sel[None].contiguous(), st.sel_count[None].contiguous())
+    torch.cuda.synchronize()
+    assert (out[0][0] - st.out_o32).abs().max() <= 1e-4 and torch.allclose(out[2][0], st.out_m, rtol=1e-5, atol=1e-6)
+    # the tokens again, from a graph that advances the lengths itself
+    x = torch.empty_like(new[0])
+    b.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        b.advance()
+        tokens(b, x)
+    for i in range(steps):
+        x.copy_(new[i])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(seen[i], (bufs[0], *bufs[1])))
+
+
+@pytest.mark.gpu
+def test_pools_beyond_32_bit_offsets():
+    """Pages whose elements lie beyond 2^31 (and bytes beyond 2^32): written, attended and read where they are."""
+    import paper_2606_30389_amd as P
+    from paper_2606_30389_amd import runtime as R
+    page, tokens = 256, 700
+    pool = (1 << 31) // (page * S.D) + 40
+    ids = [pool - 1, 3, pool - 7]
+    table = torch.tensor([ids], dtype=torch.int32, device=DEV)
+    pc = R.PathConfig(num_q_heads=4, num_kv_heads=1, page_size=page, num_tokens=pool * page, k_select=1, max_pages=pool)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    qkv = torch.randn(tokens, 6, S.D, generator=g, device=DEV).to(torch.bfloat16)
+    q, k, v = qkv[:, :4], qkv[:, 4:5], qkv[:, 5:]
+    slot = (torch.tensor(ids)[torch.arange(tokens) // page] * page + torch.arange(tokens) % page).to(DEV)
+    for kind in ("16", "e4m3"):
+        cache = R.PagedCache(pc, DEV, kind=kind)
+        b = R.Batch(DEV, [tokens], [tokens], table)
+        qr = cache.append(b, q, k, v)
+        assert torch.equal(qr, q)
+        one = R.Batch(DEV, [1], [tokens], table)
+        out = cache.attend(one, qr[-1:])
+        if kind == "16":
+            assert torch.equal(cache.k.view(-1, S.D)[slot], k[:, 0]) and torch.equal(cache.v.view(-1, S.D)[slot], v[:, 0])
+            o, _, _ = cache.prompt(b, qr)
+            kk, vv = k, v
+            want = causal64(q.double(), k.double(), v.double(), 0)
+            assert (o.double().flatten(0, 1) - want[0]).abs().max() <= 4 * 2.0 ** -8 * want[3].max()
+        else:
+            kk, vv = (t[0].flatten(0, 1)[:tokens, None] for t in cache.read(tokens, table[0]))
+            assert (kk.double() - k.double()).abs().max() <= 2.0 ** -4 * k.abs().max()
+        want = causal64(q[-1:].double(), kk.double(), vv.double(), tokens - 1)
+        assert (out[0][0].double() - want[0]).abs().max() <= 1e-4
+        del cache
+        torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+def test_two_streams_at_once():
+    """Prompts and single tokens over one cache from two streams at the same time, outputs and workspaces made by the
+    calls."""
+    from paper_2606_30389_amd import runtime as R
+    pc = R.PathConfig(num_q_heads=8, num_kv_heads=2, page_size=16, num_tokens=8000, k_select=1)
+    cache = R.PagedCache(pc, DEV)
+    g = torch.Generator(device=DEV).manual_seed(5)
+    cache.k.copy_(torch.randn(cache.k.shape, generator=g, device=DEV))
+    cache.v.copy_(torch.randn(cache.v.shape, generator=g, device=DEV))
+    q = torch.randn(30, 8, S.D, generator=g, device=DEV).to(torch.bfloat16)
+    prompt, one = R.Batch(DEV, [30], [8000]), R.Batch(DEV, [1], [7777])
+    want = cache.prompt(prompt, q), cache.attend(one, q[:1])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(10):
+        for s in streams:
+            got.append((cache.prompt(prompt, q, stream=s), cache.attend(one, q[:1], stream=s)))
+    torch.cuda.synchronize()
+    for p, a in got:
+        assert all(torch.equal(x, y) for x, y in zip(p, want[0])) and all(torch.equal(x, y) for x, y in zip(a, want[1]))
+    # a stream given by its address
+    p = cache.prompt(prompt, q, stream=streams[0].cuda_stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(p, want[0]))
