@@ -68,7 +68,8 @@ prr::BatchArgs batch_args(const prr_batch* b) {
   a.kv_len = b->kv_len;
   a.page_table = b->page_table;
   a.n_seqs = b->n_seqs;
-  a.total_q = b->total_q;
+  // rows that a sequence can have: the device cuts cu_q to them
+  a.total_q = b->cu_q ? (int)std::min((int64_t)b->total_q, (int64_t)b->n_seqs * b->max_q) : b->n_seqs;
   a.max_q = b->max_q;
   a.max_kv = b->max_kv;
   a.table_stride = b->table_stride;
@@ -131,6 +132,9 @@ prr_status plan(const prr_dims* d, const prr_batch* b, prr::PromptLaunch& a) {
   a.max_pages = d->max_pages;
   a.page_shift = log2_of(d->page_size);
   a.bf16 = d->dtype == PRR_BF16;
+  // (128 GiB of queries; keeps the grid's threads below 2^32)
+  if ((int64_t)a.b.total_q * d->num_q_heads > ((int64_t)1 << 29))
+    return api_fail(PRR_ERR_UNSUPPORTED, "%d rows x %d heads: more than 2^29", a.b.total_q, d->num_q_heads);
   prr::plan_prompt(a);
   return PRR_OK;
 }
@@ -156,11 +160,9 @@ prr_status plan(const prr_dims* d, const prr_batch* b, int32_t kind, int32_t cap
   return PRR_OK;
 }
 
-int64_t part_rows(const prr_dims* d, const prr_batch* b, const prr::PromptLaunch&) {
-  return (int64_t)b->total_q * d->num_q_heads;
-}
-int64_t part_rows(const prr_dims* d, const prr_batch* b, const prr::DecodeLaunch&) {
-  return (int64_t)b->n_seqs * d->num_q_heads;
+template <class A>
+int64_t part_rows(const prr_dims* d, const A& a) {
+  return (int64_t)a.b.total_q * d->num_q_heads;
 }
 
 }  // namespace
@@ -258,6 +260,7 @@ prr_status prr_rope_append(const prr_dims* dims, const prr_batch* batch, const v
   a.bf16 = dims->dtype == PRR_BF16;
   a.e4m3 = kv_kind == PRR_KV_E4M3;
   a.interleaved = layout == PRR_ROPE_INTERLEAVED;
+  if (a.b.total_q == 0) return api_ok();  // (no sequence has a new token)
   return hip_status(prr::launch_rope_append(a, stream), "rope append");
 }
 
@@ -293,7 +296,7 @@ prr_status prr_cache_read(const prr_dims* dims, const void* k_codes, const void*
 size_t prr_prompt_workspace_size(const prr_dims* dims, const prr_batch* batch) {
   prr::PromptLaunch a;
   if (plan(dims, batch, a) != PRR_OK) return 0;
-  return parts_bytes(part_rows(dims, batch, a), a.nsplit);
+  return parts_bytes(part_rows(dims, a), a.nsplit);
 }
 
 prr_status prr_prompt_attn(const prr_dims* dims, const prr_batch* batch, const void* q, const void* k_cache,
@@ -310,7 +313,7 @@ prr_status prr_prompt_attn(const prr_dims* dims, const prr_batch* batch, const v
     PRR_TRY(prr::api_check_ptr(out_m, "out_m", 4));
     PRR_TRY(prr::api_check_ptr(out_l, "out_l", 4));
   }
-  const int64_t rows = part_rows(dims, batch, a);
+  const int64_t rows = part_rows(dims, a);
   PRR_TRY(check_ws(workspace, ws_bytes, parts_bytes(rows, a.nsplit)));
   a.q = q;
   a.k = k_cache;
@@ -327,7 +330,7 @@ prr_status prr_prompt_attn(const prr_dims* dims, const prr_batch* batch, const v
 size_t prr_decode_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t kv_kind, int32_t cap) {
   prr::DecodeLaunch a;
   if (plan(dims, batch, kv_kind, cap, a) != PRR_OK) return 0;
-  return parts_bytes(part_rows(dims, batch, a), a.nsplit);
+  return parts_bytes(part_rows(dims, a), a.nsplit);
 }
 
 prr_status prr_decode_attn(const prr_dims* dims, const prr_batch* batch, const void* q, int32_t kv_kind,
@@ -348,7 +351,7 @@ prr_status prr_decode_attn(const prr_dims* dims, const prr_batch* batch, const v
   if (out_o) PRR_TRY(prr::api_check_ptr(out_o, "out_o", 8));
   PRR_TRY(prr::api_check_ptr(out_m, "out_m", 4));
   PRR_TRY(prr::api_check_ptr(out_l, "out_l", 4));
-  const int64_t rows = part_rows(dims, batch, a);
+  const int64_t rows = part_rows(dims, a);
   PRR_TRY(check_ws(workspace, ws_bytes, parts_bytes(rows, a.nsplit)));
   a.q = q;
   a.pages = pages;

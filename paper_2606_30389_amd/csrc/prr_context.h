@@ -57,7 +57,7 @@ struct PromptLaunch {
   BatchArgs b;
   int num_kv_heads, group, max_pages, page_shift;
   int tiles;   // upper bound of the row tiles of one KV head
-  int nsplit;  // parts of a row tile's keys
+  int nsplit, part_tiles;  // parts of a row tile's keys, of so many tiles of 64 tokens
   int waves;   // of a workgroup, 32 rows each
   bool bf16;
 };

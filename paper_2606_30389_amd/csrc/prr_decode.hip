@@ -173,7 +173,10 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
   __shared__ __align__(16) DecodeLds S;
   const int t = threadIdx.x, lane = lane_id(), w = __builtin_amdgcn_readfirstlane(t / kWave);
   const int j = lane >> 4, n = lane & 15;
-  const int part = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
+  const int h = blockIdx.y, s = blockIdx.z;
+  // (workgroups go to the XCDs in turn: without the shift the first parts, all that short sequences have,
+  // would fall on one XCD where nsplit is a multiple of 8)
+  const int part = (int)(blockIdx.x + h + s) % a.nsplit;
   const int G = a.group;
   const float kNegInf = -__builtin_inff();
   const int kv = min(max(a.b.kv_len[s], 0), a.b.max_kv);
@@ -384,9 +387,12 @@ void plan_decode(DecodeLaunch& a) {
   const int64_t units = (int64_t)a.b.n_seqs * a.c.num_kv_heads;
   // Parts of 64 tiles (eight a wave: less, and starting and merging parts outweighs them; 512 parts of
   // 32 tiles for 2 x 8192: 27.8 us, 256 of 64: 21.0) or of the share of 512 workgroups, two a CU; where that
-  // leaves CUs idle, as many parts as CUs, of a tile a wave at least.
+  // leaves CUs idle, as many parts as CUs, of a tile a wave at least.  Lengths are bounds here: parts
+  // of at most 256 tiles keep one long sequence among short ones from being one workgroup's (64 sequences x 8
+  // KV heads, one of 131072 tokens and 63 of 500: 191 us instead of 1383), unless that takes more than 65536 workgroups,
+  // most of which would find nothing to do.
   const int64_t all = tiles * units;
-  int64_t per = max((int64_t)64, (all + 511) / 512);
+  int64_t per = max((int64_t)64, min((all + 511) / 512, max((int64_t)256, all / 65536)));
   if (all < 64 * 256) per = (all + 255) / 256;
   per = (min(per, tiles) + NW - 1) / NW * NW;
   a.tiles_per_split = (int)per;

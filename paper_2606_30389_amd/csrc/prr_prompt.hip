@@ -126,8 +126,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
   const int wave_lo = first + min(row0 + 32 * w, rows - 1) / G;
   const int keys = max(0, first + min(row0 + kRows - 1, rows - 1) / G + 1);
   const int ntiles = (keys + kTokens - 1) / kTokens;
-  const int per = (ntiles + a.nsplit - 1) / a.nsplit;
-  const int t0 = min(part * per, ntiles), t1 = min(t0 + per, ntiles);
+  const int t0 = min(part * a.part_tiles, ntiles), t1 = min(t0 + a.part_tiles, ntiles);
 
   const int partial = (first + row0 / G + 1) / kTokens;  // tiles from this one on are not seen whole by every row
   if (t == 0) any_bad = 0;
@@ -397,12 +396,14 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
   } else if (live) {
     const int64_t x = (int64_t)part * a.b.total_q * a.num_kv_heads * G + out_row;
     float* o = a.part_o + x * kHeadDim + 4 * hf;
+    if (t0 < t1) {  // (the outputs of an empty part are not read)
 #pragma unroll
-    for (int cb = 0; cb < 4; ++cb)
+      for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(o + 32 * cb + 2 * i) =
-            make_float4(acc[cb][i] * inv, acc[cb][i + 1] * inv, acc[cb][i + 2] * inv, acc[cb][i + 3] * inv);
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<float4*>(o + 32 * cb + 2 * i) =
+              make_float4(acc[cb][i] * inv, acc[cb][i + 1] * inv, acc[cb][i + 2] * inv, acc[cb][i + 3] * inv);
+    }
     if (hf == 0) {
       a.part_ml[2 * x] = mx;
       a.part_ml[2 * x + 1] = exact;
@@ -410,30 +411,48 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
   }
 }
 
-// The parts of a row: 32 threads a row, four channels each.
-template <bool BF16>
+// The parts of a row: 32 threads hold its channels, four each; GROUPS such groups share the row's parts.
+template <bool BF16, int GROUPS>
 __global__ __launch_bounds__(256) void merge_prompt_kernel(const PromptLaunch a) {
+  __shared__ __align__(16) float so[GROUPS][kHeadDim], sl[GROUPS];
   const int64_t rows = (int64_t)a.b.total_q * a.num_kv_heads * a.group;
-  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int grp = GROUPS == 1 ? 0 : threadIdx.x >> 5;
+  const int64_t row = GROUPS == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x;
   const int c4 = (threadIdx.x & 31) * 4;
   const float kNegInf = -__builtin_inff();
   const int end = a.b.cu_q ? min(a.b.cu_q[a.b.n_seqs], a.b.total_q) : a.b.n_seqs;
   if (row >= (int64_t)end * a.num_kv_heads * a.group) return;
   float mx = kNegInf;
+#pragma unroll 8
   for (int p = 0; p < a.nsplit; ++p) mx = fmaxf(mx, a.part_ml[2 * (p * rows + row)]);
   float sum = 0.0f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int p = 0; p < a.nsplit; ++p) {
+#pragma unroll 4
+  for (int p = grp; p < a.nsplit; p += GROUPS) {
     const int64_t at = p * rows + row;
-    const float m = a.part_ml[2 * at], l = a.part_ml[2 * at + 1];
-    const float4 y = *reinterpret_cast<const float4*>(a.part_o + at * kHeadDim + c4);
-    const float f = m == kNegInf ? 0.0f : l * exp2_hw((m - mx) * kSoftmaxScale2);
-    if (f != 0.0f) {
-      sum += f;
-      o.x += f * y.x;
-      o.y += f * y.y;
-      o.z += f * y.z;
-      o.w += f * y.w;
+    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * at);
+    const float f = ml.x == kNegInf ? 0.0f : ml.y * exp2_hw((ml.x - mx) * kSoftmaxScale2);
+    // (an empty part has no output: the first part's is read instead, which there always is)
+    const float4 y = *reinterpret_cast<const float4*>(a.part_o + (ml.x == kNegInf ? row : at) * kHeadDim + c4);
+    sum += f;
+    o.x += f != 0.0f ? f * y.x : 0.0f;
+    o.y += f != 0.0f ? f * y.y : 0.0f;
+    o.z += f != 0.0f ? f * y.z : 0.0f;
+    o.w += f != 0.0f ? f * y.w : 0.0f;
+  }
+  if constexpr (GROUPS > 1) {
+    *reinterpret_cast<float4*>(&so[grp][c4]) = o;
+    if (c4 == 0) sl[grp] = sum;
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int x = 1; x < GROUPS; ++x) {
+      const float4 y = *reinterpret_cast<const float4*>(&so[x][c4]);
+      sum += sl[x];
+      o.x += y.x;
+      o.y += y.y;
+      o.z += y.z;
+      o.w += y.w;
     }
   }
   const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
@@ -453,16 +472,22 @@ void plan_prompt(PromptLaunch& a) {
     const int64_t each = (int64_t)a.b.n_seqs * (((int64_t)a.b.max_q * a.group + rows - 1) / rows);
     return min(packed, each);
   };
-  // fewer workgroups than CUs: the keys are cut into parts of at least eight tiles, as many as fill the
-  // chip once (twice as many small parts fill it better, but joining them and power take that back)
-  const int64_t key_tiles = ((int64_t)a.b.max_kv + kTokens - 1) / kTokens;
-  const auto parts_of = [&](int64_t units) {
-    return (int)max((int64_t)1, min((int64_t)256 / max(units, (int64_t)1), key_tiles / 8));
+  const int64_t key_tiles = max(((int64_t)a.b.max_kv + kTokens - 1) / kTokens, (int64_t)1);
+  // Parts of a row tile's keys.  Fewer workgroups than CUs: as many parts, of at least eight tiles, as fill
+  // the chip once (twice as many small ones fill it better, but joining them and power take that back).
+  // Enough workgroups, but so few that one sequence with many more keys than the others could outlast them
+  // all: parts of 512 tiles, eight at most, for 1.5% (16 new tokens of 64 sequences, one of 131072 tokens
+  // and 63 of 500, 32 / 8 heads: 2812 us in one part, 766 in four).
+  const auto parts_of = [&](int64_t units) -> int64_t {
+    if (units <= 256) return max((int64_t)1, min(256 / max(units, (int64_t)1), key_tiles / 8));
+    return units < 4096 ? min((key_tiles + 511) / 512, (int64_t)8) : 1;
   };
   const int64_t units = tiles_of(256) * a.num_kv_heads;
   a.waves = units <= 128 && parts_of(units) == 1 ? 4 : 8;
   a.tiles = (int)tiles_of(32 * a.waves);
-  a.nsplit = parts_of((int64_t)a.tiles * a.num_kv_heads);
+  const int64_t parts = parts_of((int64_t)a.tiles * a.num_kv_heads);
+  a.part_tiles = (int)((key_tiles + parts - 1) / parts);
+  a.nsplit = (int)((key_tiles + a.part_tiles - 1) / a.part_tiles);
 }
 
 namespace {
@@ -481,7 +506,10 @@ hipError_t launch_prompt(const PromptLaunch& a, hipStream_t stream) {
   const hipError_t e = launch_one(f, dim3(a.tiles * a.num_kv_heads, a.nsplit), a.waves * kWave, stream, a);
   if (e != hipSuccess || a.nsplit == 1) return e;
   const int64_t rows = (int64_t)a.b.total_q * a.num_kv_heads * a.group;
-  return launch_one(a.bf16 ? (const void*)merge_prompt_kernel<true> : (const void*)merge_prompt_kernel<false>,
+  if (a.nsplit > 8)  // (few rows)
+    return launch_one(a.bf16 ? (const void*)merge_prompt_kernel<true, 8> : (const void*)merge_prompt_kernel<false, 8>,
+                      dim3((unsigned)rows), 256, stream, a);
+  return launch_one(a.bf16 ? (const void*)merge_prompt_kernel<true, 1> : (const void*)merge_prompt_kernel<false, 1>,
                     dim3((unsigned)((rows + 7) / 8)), 256, stream, a);
 }
 

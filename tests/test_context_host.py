@@ -194,6 +194,15 @@ def test_cache_read_refusals(P):
 
 def test_no_new_tokens_is_no_work(P):
     prompt(P, b=batch(P, max_q=0))()
+    rope(P, b=batch(P, max_q=0))()
+
+
+def test_workspaces_follow_the_rows_that_can_be_live(P):
+    d = dims(P, max_pages=1 << 12)
+    few = dict(n_seqs=1, max_q=4, max_kv=1 << 16, table_stride=1 << 12)
+    assert P.prr_prompt_workspace_size(d, batch(P, total_q=4, **few)) == P.prr_prompt_workspace_size(d, batch(P, total_q=1 << 24, **few))
+    _expect(P, P.PRR_ERR_UNSUPPORTED, prompt(P, d=dims(P, num_q_heads=256, num_kv_heads=256),
+                                             b=batch(P, n_seqs=4096, total_q=1 << 24, max_q=1 << 20, table_stride=1 << 12)))
 
 
 # ------------------------------------------------------------------------------- frequencies
