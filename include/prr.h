@@ -10,6 +10,10 @@
  *   repair   prr_repair       attend the missed pages A \ P and merge, so the result
  *                             is attention over exactly A (or over P u A, on request)
  *
+ * Around it, for one or many sequences: prr_rope_append writes new tokens into the paged cache
+ * with their rotary positions (16 bits or e4m3), prr_prompt_attn attends prompts, prr_decode_attn
+ * whole caches, prr_cache_read gives e4m3 pages back in 16 bits.
+ *
  * Citations name sections, equations and the appendix of "Predict, Reuse, and
  * Repair: Accelerating Dynamic Sparse Attention for Long-Context LLM Decoding".
  *
@@ -266,7 +270,9 @@ prr_status prr_repair(const prr_dims* dims, const void* q, const void* k_cache, 
  *                identity (n_seqs = 1).  Entries at or behind a sequence's last page are not
  *                read.  An entry outside [0, max_pages) is never dereferenced.  No page may
  *                hold two sequences' new tokens
- * Device values beyond what max_q, max_kv and total_q say are cut to them. */
+ * Device values beyond what max_q, max_kv and total_q say are cut to them: nothing outside the
+ * arguments is touched, but a longer sequence's results are not its own.  Lengths may change
+ * between calls, and between replays of a captured graph, within those bounds. */
 typedef struct {
   int32_t n_seqs;
   int32_t total_q;
@@ -284,7 +290,8 @@ typedef struct {
  * PRR_KV_E4M3: e4m3 codes (finite, no infinities: 448 the largest) of that layout, and one
  * scale byte per row, [Hkv][max_pages][page_size] uint8: the row's numbers are
  * code * 2^(byte - 127), byte in 1..254.  A power of two costs no accuracy (a float's relative
- * step does not depend on its exponent) and reading back multiplies exactly. */
+ * step does not depend on its exponent) and reading back multiplies exactly.  Caches and scale
+ * arrays are 16-byte aligned. */
 #define PRR_KV_16 0
 #define PRR_KV_E4M3 1
 
@@ -343,7 +350,8 @@ prr_status prr_rope_append(const prr_dims* dims, const prr_batch* batch, const v
 
 /* Pages of an e4m3 cache in 16 bits: logical pages [page_begin, page_end) of a sequence of
  * num_tokens tokens.
- *   page_table   device int32 logical -> physical page, or NULL = identity
+ *   page_table   device int32 logical -> physical page (entries [page_begin, page_end) are
+ *                read), or NULL = identity
  *   k_out, v_out device [Hkv][page_end - page_begin][page_size][128] dtype out: a cache of its
  *                own (identity table, max_pages = page_end - page_begin) for the calls above.
  *                Tokens at or behind num_tokens, and pages whose entry is outside
@@ -361,7 +369,8 @@ prr_status prr_cache_read(const prr_dims* dims, const void* k_codes, const void*
  *   out_o        device [total_q][Hq][128] dtype out
  *   out_m, out_l device [total_q][Hq] float32 out (both or neither NULL)
  * Weights are rounded to the 16-bit type for the product with the values, everything else is
- * float32.  A token that sees no key gets the empty state.  A page-table entry out of range
+ * float32.  A token that sees no key gets the empty state.  Keys and values that a token does not
+ * see do not change its result, infinities and NaN among them.  A page-table entry out of range
  * makes the results of its sequence unspecified.  Workspace: prr_prompt_workspace_size bytes,
  * 256-byte aligned, contents of no account before and after (NULL if that is 0). */
 size_t prr_prompt_workspace_size(const prr_dims* dims, const prr_batch* batch);

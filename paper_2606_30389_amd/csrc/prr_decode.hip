@@ -21,7 +21,7 @@ namespace {
 // An e4m3 cache: codes are exact in either 16-bit type.  q.code is scaled by the key's power of two
 // in float32.  The value's power of two 2^ev joins the weight, p 2^ev = 2^(x + ev - y), y the largest
 // x + ev so far (x the logit in powers of two): every weight that counts is near 1, whatever the
-// scales, and the product runs in float16, whose two-term weights carry 22 bits (bfloat16's: 17).
+// scales, and the product runs in float16, whose two-term weights carry 22 bits.
 constexpr int NW = 8;  // waves of a workgroup
 constexpr int kTile = 16;
 constexpr float kNoRef = -3e38f;  // nothing seen yet: 2^(kNoRef - anything later) = 0
@@ -137,7 +137,7 @@ __device__ __forceinline__ void attend_tile(const TileData<E4M3>& d, const u32x4
                      unpack_codes<false, false>(d.v[i][1], 1.0f), unpack_codes<false, true>(d.v[i][1], 1.0f)};
     pv_tile<false>(st.acc, v, w);
   } else {
-    pv_tile<BF16>(st.acc, d.v, w);
+    pv_tile<BF16, BF16 ? 3 : 2>(st.acc, d.v, w);  // (two bfloat16 terms: an error of 2e-6 where float32 has 1e-6)
   }
 }
 

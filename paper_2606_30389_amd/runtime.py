@@ -17,7 +17,6 @@ All arithmetic happens in libprr.so; this module only allocates, uploads and ord
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import dataclasses
 from typing import List, Optional, Sequence
@@ -98,26 +97,46 @@ class Batch:
     reads them; max_q and max_kv bound them for as long as the batch is used."""
 
     def __init__(self, device, new: Sequence[int], kv: Sequence[int], page_table=None, max_q=None, max_kv=None, total_q=None):
+        if len(new) != len(kv) or not len(new) or min(new) < 0 or min(kv) < 0:
+            raise ValueError("new and kv: lengths of the same sequences, at least one, none negative")
         cu = np.concatenate([[0], np.cumsum(np.asarray(new, dtype=np.int64))]).astype(np.int32)
+        self._longest, self._max_kv = max(kv), max(kv) if max_kv is None else max_kv
         self.kv_len = torch.tensor(list(kv), dtype=torch.int32, device=device)
         self.page_table = page_table
         # one new token each: rows are sequences
         self.cu_q = None if all(n == 1 for n in new) else torch.from_numpy(cu).to(device)
         self.total_q = int(cu[-1]) if total_q is None else total_q
         self.native = L.make_batch(len(self.kv_len), self.total_q, max(new) if max_q is None else max_q,
-                                   max(kv) if max_kv is None else max_kv, self.cu_q, self.kv_len, page_table,
+                                   self._max_kv, self.cu_q, self.kv_len, page_table,
                                    0 if page_table is None else page_table.shape[-1])
 
+    def set_lengths(self, kv: Sequence[int]):
+        """Tokens of each sequence in the cache from now on (on the current stream)."""
+        if len(kv) != len(self.kv_len) or min(kv) < 0 or max(kv) > self._max_kv:
+            raise ValueError(f"{len(self.kv_len)} lengths within [0, {self._max_kv}] are needed")
+        self.kv_len.copy_(torch.tensor(list(kv), dtype=torch.int32))
+        self._longest = max(kv)
+
     def advance(self):
-        """Every sequence is one token longer (on the current stream)."""
+        """Every sequence is one token longer (on the current stream).  Replays of a captured graph that holds
+        this are not counted here: max_kv has to leave room for them."""
+        if self._longest >= self._max_kv:
+            raise ValueError(f"a sequence of {self._longest} tokens cannot grow beyond max_kv {self._max_kv}")
+        self._longest += 1
         self.kv_len.add_(1)
 
 
-def _stream_context(stream):
-    """What is allocated inside belongs to `stream` (None: the current one), as the kernels that write it."""
+def _stream_context(stream, device):
+    """What is allocated inside belongs to `stream` (None: the device's current one), as the kernels that write it."""
     if stream is None:
-        return contextlib.nullcontext()
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+        return torch.cuda.device(device)
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream)
+
+
+def _check_rows(x, name, heads, dtype, dense):
+    if x.dtype != dtype or x.dim() != 3 or tuple(x.shape[1:]) != (heads, 128) or (dense and not x.is_contiguous()):
+        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}, strides {x.stride()}; expected {'dense ' if dense else ''}"
+                         f"{dtype} [rows][{heads}][128]")
 
 
 class PagedCache:
@@ -151,8 +170,11 @@ class PagedCache:
 
     def append(self, batch: Batch, q, k, v, rope: Optional[Rope] = None, positions=None, q_out=None, stream=None):
         """New tokens' keys and values into the cache, rotated; returns the rotated queries."""
+        for x, name, heads in ((q, "q", self.cfg.num_q_heads), (k, "k", self.cfg.num_kv_heads), (v, "v", self.cfg.num_kv_heads)):
+            if x is not None:
+                _check_rows(x, name, heads, self.cfg.torch_dtype, False)
         if q is not None and q_out is None:
-            with _stream_context(stream):
+            with _stream_context(stream, self.k.device):
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         L.prr_rope_append(self.dims, batch.native, q, k, v, positions, None if rope is None else rope.freqs,
                           0 if rope is None else rope.rot_dim, L.PRR_ROPE_HALF if rope is None else rope.layout,
@@ -164,8 +186,9 @@ class PagedCache:
         """Causal attention of the new tokens: (o in the 16-bit type, m, l)."""
         if self.kind != L.PRR_KV_16:
             raise ValueError("prompts attend a 16-bit cache: read() the pages back first")
+        _check_rows(q, "q", self.cfg.num_q_heads, self.cfg.torch_dtype, True)
         nbytes = L.prr_prompt_workspace_size(self.dims, batch.native)
-        with _stream_context(stream):
+        with _stream_context(stream, self.k.device):
             if out is None:
                 n, hq = q.shape[:2]
                 out = (torch.zeros_like(q), *(torch.zeros(n, hq, dtype=torch.float32, device=q.device) for _ in range(2)))
@@ -176,9 +199,10 @@ class PagedCache:
     def attend(self, batch: Batch, q, pages=None, counts=None, out=None, stream=None):
         """Attention of one token per sequence over its whole cache, or over listed pages
         ([sequence][KV head][cap] and [sequence][KV head]): (o float32, o in the 16-bit type, m, l)."""
+        _check_rows(q, "q", self.cfg.num_q_heads, self.cfg.torch_dtype, True)
         cap = 0 if pages is None else pages.shape[-1]
         nbytes = L.prr_decode_workspace_size(self.dims, batch.native, self.kind, cap)
-        with _stream_context(stream):
+        with _stream_context(stream, self.k.device):
             if out is None:
                 n, hq = q.shape[:2]
                 f32 = dict(dtype=torch.float32, device=q.device)
@@ -194,7 +218,7 @@ class PagedCache:
             page_end = -(-num_tokens // self.cfg.page_size)
         if out is None:
             shape = (self.cfg.num_kv_heads, page_end - page_begin, self.cfg.page_size, 128)
-            with _stream_context(stream):
+            with _stream_context(stream, self.k.device):
                 out = tuple(torch.zeros(shape, dtype=self.cfg.torch_dtype, device=self.k.device) for _ in range(2))
         L.prr_cache_read(self.dims, self.k, self.v, self.k_scale, self.v_scale, page_table, num_tokens, page_begin, page_end,
                          *out, stream)

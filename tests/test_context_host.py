@@ -205,6 +205,27 @@ def test_workspaces_follow_the_rows_that_can_be_live(P):
                                              b=batch(P, n_seqs=4096, total_q=1 << 24, max_q=1 << 20, table_stride=1 << 12)))
 
 
+def test_batches_of_the_runtime_are_checked():
+    from paper_2606_30389_amd import runtime as R
+    for new, kv in (([1], [1, 2]), ([], []), ([-1], [4]), ([1], [-4])):
+        with pytest.raises(ValueError):
+            R.Batch("cpu", new, kv)
+    b = R.Batch("cpu", [1, 1], [3, 4], max_kv=5)
+    assert b.cu_q is None and b.total_q == 2 and b.native.max_kv == 5
+    b.advance()
+    with pytest.raises(ValueError):
+        b.advance()
+    assert b.kv_len.tolist() == [4, 5]
+    for kv in ([1], [1, 6], [-1, 2]):
+        with pytest.raises(ValueError):
+            b.set_lengths(kv)
+    b.set_lengths([0, 1])
+    b.advance()
+    assert b.kv_len.tolist() == [1, 2]
+    p = R.Batch("cpu", [3, 0, 2], [3, 5, 9])
+    assert p.cu_q.tolist() == [0, 3, 3, 5] and p.native.max_q == 3 and p.native.total_q == 5
+
+
 # ------------------------------------------------------------------------------- frequencies
 
 @pytest.mark.parametrize("rot", [4, 64, 96, 128])

@@ -147,7 +147,7 @@ def test_quantised_batch_generates():
     assert (out[0][0] - st.out_o32).abs().max() <= 1e-4 and torch.allclose(out[2][0], st.out_m, rtol=1e-5, atol=1e-6)
     # the tokens again, from a graph that advances the lengths itself
     x = torch.empty_like(new[0])
-    b.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+    b.set_lengths(lens)
     graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
     torch.cuda.synchronize()
     with torch.cuda.graph(graph, stream=stream):

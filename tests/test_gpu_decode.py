@@ -78,8 +78,9 @@ class Case:
         G, b = self.hq // self.hkv, self.b
         eps = S.half_step(DT[self.dt])
         two = torch.float16 if self.kind == "e4m3" else DT[self.dt]
-        # a weight in two terms: one rounding of the rest of one rounding; float16: subnormal below 2^-24
-        werr, floor = S.half_step(two) ** 2, 2.0 ** -25 if two == torch.float16 else 0.0
+        # a weight in two float16 terms: one rounding of the rest of one rounding, subnormal below 2^-24; in three
+        # bfloat16 ones: one more
+        werr, floor = (S.half_step(two) ** 2, 2.0 ** -25) if two == torch.float16 else (S.half_step(two) ** 3, 0.0)
         for s, kv in enumerate(b.kv):
             for h in range(self.hkv):
                 pos = torch.arange(kv)
