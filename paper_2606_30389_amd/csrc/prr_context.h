@@ -59,6 +59,7 @@ struct PromptLaunch {
   int tiles;   // upper bound of the row tiles of one KV head
   int nsplit, part_tiles;  // parts of a row tile's keys, of so many tiles of 64 tokens
   int waves;   // of a workgroup, 32 rows each
+  uint32_t magic;  // divides by the group size
   bool bf16;
 };
 

@@ -32,8 +32,9 @@ namespace {
 // power bounds it, and schedules with fewer stalls but more instructions (four sums and maxima side by
 // side, operands read further ahead) come out 1-3% slower.
 //
-// Four waves a workgroup (one per SIMD, nothing to take turns with) where a call is so short that
-// 256-row tiles leave half of the CUs idle and the keys are too few to be split.
+// Up to 1024 tokens, four waves a workgroup, two workgroups a CU, which start and end (about 9 us a
+// workgroup) under each other's work instead of taking turns: 32 sequences of 512 tokens, 32 / 8 heads, 140 us
+// (eight waves: 152), 1024 tokens 29 (39); 2048 tokens 61 (58), 16384 tokens 2118 (1916).
 constexpr int kTokens = 64;
 constexpr int kKPitch = kHeadDim + 8, kVPitch = kHeadDim + 32;  // elements
 constexpr float kNoRef = -3e38f;
@@ -71,6 +72,9 @@ __device__ __forceinline__ float sum_halves(float v) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// x / G for 0 <= x < 2^28 (G <= 16): magic = ceil(2^32 / G), off by less than G / 2^32 of x; 0 stands for G = 1
+__device__ __forceinline__ int over_group(int x, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)x, magic) : x; }
+
 // The sequence and the row tile in it of tile number `tile` of the batch; false: no such tile.
 __device__ __forceinline__ bool find_tile(const PromptLaunch& a, int rows, int tile, int& s, int& local, Seq& sq) {
   const auto tiles_of = [&](const Seq& x) { return ((x.q1 - x.q0) * a.group + rows - 1) / rows; };
@@ -84,13 +88,16 @@ __device__ __forceinline__ bool find_tile(const PromptLaunch& a, int rows, int t
   int base = 0;
   for (int s0 = 0; s0 < a.b.n_seqs; s0 += kWave) {
     const int x = s0 + lane_id();
-    const int n = x < a.b.n_seqs ? tiles_of(seq_at(a.b, x)) : 0;
-    const int inc = wave_inclusive_scan(n);
+    Seq mine = {0, 0, 0};
+    if (x < a.b.n_seqs) mine = seq_at(a.b, x);
+    const int inc = wave_inclusive_scan(tiles_of(mine));
     const uint64_t past = __ballot(base + inc > tile);
     if (past) {
       const int at = __builtin_ctzll(past);
       s = s0 + at;
-      sq = seq_at(a.b, s);
+      sq.q0 = __builtin_amdgcn_readlane(mine.q0, at);
+      sq.q1 = __builtin_amdgcn_readlane(mine.q1, at);
+      sq.kv = __builtin_amdgcn_readlane(mine.kv, at);
       // the last rows of a sequence have the most keys: they are taken first
       local = base + __builtin_amdgcn_readlane(inc, at) - 1 - tile;
       return true;
@@ -121,14 +128,14 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
   // this lane's row, the positions of the wave's rows, and the keys that the workgroup needs
   const int row = min(row0 + 32 * w + n, rows - 1);
   const bool live = row0 + 32 * w + n < rows;
-  const int tok = row / G, head = row - tok * G;
+  const int tok = over_group(row, a.magic), head = row - tok * G;
   const int pos = first + tok;
-  const int wave_lo = first + min(row0 + 32 * w, rows - 1) / G;
-  const int keys = max(0, first + min(row0 + kRows - 1, rows - 1) / G + 1);
+  const int wave_lo = first + over_group(min(row0 + 32 * w, rows - 1), a.magic);
+  const int keys = max(0, first + over_group(min(row0 + kRows - 1, rows - 1), a.magic) + 1);
   const int ntiles = (keys + kTokens - 1) / kTokens;
   const int t0 = min(part * a.part_tiles, ntiles), t1 = min(t0 + a.part_tiles, ntiles);
 
-  const int partial = (first + row0 / G + 1) / kTokens;  // tiles from this one on are not seen whole by every row
+  const int partial = (first + over_group(row0, a.magic) + 1) / kTokens;  // tiles from this one on are not seen whole by every row
   if (t == 0) any_bad = 0;
   if (TURNS) __syncthreads();  // (else the first barrier below comes before the first values)
 
@@ -482,8 +489,8 @@ void plan_prompt(PromptLaunch& a) {
     if (units <= 256) return max((int64_t)1, min(256 / max(units, (int64_t)1), key_tiles / 8));
     return units < 4096 ? min((key_tiles + 511) / 512, (int64_t)8) : 1;
   };
-  const int64_t units = tiles_of(256) * a.num_kv_heads;
-  a.waves = units <= 128 && parts_of(units) == 1 ? 4 : 8;
+  a.waves = key_tiles <= 16 ? 4 : 8;
+  a.magic = a.group == 1 ? 0u : (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
   a.tiles = (int)tiles_of(32 * a.waves);
   const int64_t parts = parts_of((int64_t)a.tiles * a.num_kv_heads);
   a.part_tiles = (int)((key_tiles + parts - 1) / parts);
