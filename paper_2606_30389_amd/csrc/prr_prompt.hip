@@ -236,16 +236,16 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
     const int buf = (tile - t0) & 1;
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int cb = 0; cb < 4; ++cb) pv_step(buf ^ 1, x, cb);
-#pragma unroll
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[b][i] = 0.0f;
 #pragma unroll
       for (int x = 0; x < 8; ++x) qk_step(sc, buf, b, x);
     }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) pv_step(buf ^ 1, x, cb);
     asm volatile("" : "+v"(sc[0]), "+v"(sc[1]), "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
     __builtin_amdgcn_s_setprio(0);
   };
