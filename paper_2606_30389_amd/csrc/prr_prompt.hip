@@ -28,9 +28,9 @@ namespace {
 // second half of the waves runs one phase behind the first, barriers between the phases, so that one
 // wave's products run under the other's softmax.  16384 tokens, 32 / 2 heads, bf16: 2154 us with all
 // waves in step (MFMA 46% of the cycles, VALU 45%, one after the other), 1945 in turns: 1.13 PFLOP/s,
-// where a 16384^3 library product reaches 1.38.  The clock falls from 2.15 to about 1.9 GHz meanwhile:
-// power bounds it, and schedules with fewer stalls but more instructions (four sums and maxima side by
-// side, operands read further ahead) come out 1-3% slower.
+// where a 16384^3 library product reaches 1.38.  The clock falls from 2.15 to 1.8 GHz meanwhile: power
+// bounds it, and schedules with fewer stalls but more instructions (four sums and maxima side by side,
+// operands read further ahead) come out 1-3% slower.
 //
 // Up to 1024 tokens, four waves a workgroup, two workgroups a CU, which start and end (about 9 us a
 // workgroup) under each other's work instead of taking turns: 32 sequences of 512 tokens, 32 / 8 heads, 140 us
@@ -481,7 +481,8 @@ void plan_prompt(PromptLaunch& a) {
   };
   const int64_t key_tiles = max(((int64_t)a.b.max_kv + kTokens - 1) / kTokens, (int64_t)1);
   // Parts of a row tile's keys.  Fewer workgroups than CUs: as many parts, of at least eight tiles, as fill
-  // the chip once (twice as many small ones fill it better, but joining them and power take that back).
+  // the chip once (509 new of 65536 tokens, 28 / 4 heads: 460 us in four parts, 1403 in one; twice as many small
+  // ones fill it better, but joining them and power take that back: 472 in nine).
   // Enough workgroups, but so few that one sequence with many more keys than the others could outlast them
   // all: parts of 512 tiles, eight at most, for 1.5% (16 new tokens of 64 sequences, one of 131072 tokens
   // and 63 of 500, 32 / 8 heads: 2812 us in one part, 766 in four).

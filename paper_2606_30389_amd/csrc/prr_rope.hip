@@ -14,6 +14,9 @@ namespace {
 // no lane needs another's channels, and the four angles are formed once for all rows of the token.
 // Other lanes hold 8 plain channels.  An angle is reduced in float64 to a fraction of a turn (a
 // position of 2^30 keeps 20 bits behind the point of a turn), the rest is float32.
+//
+// Bound by memory: 32768 tokens of 32 / 2 heads in 116 us, 5.2 TB/s of what has to be read and written,
+// the rate of a large copy.
 template <bool BF16, bool E4M3, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rope_append_kernel(const RopeLaunch a) {
   const int lane = lane_id();
@@ -126,7 +129,9 @@ hipError_t launch_rope(const RopeLaunch& a, int blocks, hipStream_t stream) {
 // =====================================================================================
 // an e4m3 cache's pages in 16 bits
 // =====================================================================================
-// Eight lanes per row, 16 codes each: one 16-byte load, two 16-byte stores.
+// Eight lanes per row, 16 codes each: one 16-byte load, two 16-byte stores.  The conversion multiplies by the
+// power of two and rounds once (exact but for subnormal results).  Bound by memory: 131072 tokens of two KV
+// heads in 39 us, 5.2 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(256) void cache_read_kernel(const CacheReadLaunch a) {
   const int64_t per_head = (int64_t)a.pages << a.c.page_shift, total = per_head * a.c.num_kv_heads * 8;
@@ -158,8 +163,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const CacheReadLaunch a
 hipError_t launch_rope_append(RopeLaunch a, hipStream_t stream) {
   const int rows = (a.q ? a.num_q_heads : 0) + (a.k ? 2 * a.c.num_kv_heads : 0);
   const int tokens = a.b.cu_q ? a.b.total_q : a.b.n_seqs;
-  // one wave per token forms its angles once; few tokens spread their rows over more waves, up to
-  // two per SIMD of the chip
+  // one wave per token forms its angles once (32768 tokens, 32 / 2 heads: 116 us, 173 with nine waves a
+  // token); few tokens spread their rows over more waves, up to two per SIMD of the chip (one token 2.8 us,
+  // 4.8 by one wave; 64 tokens of 32 / 8 heads 3.8, 7.9)
   a.splits = (int)min((int64_t)(rows + 3) / 4, max((int64_t)1, (int64_t)2048 / tokens));
   const int64_t waves = (int64_t)tokens * a.splits;
   const int blocks = (int)((waves + 3) / 4);
