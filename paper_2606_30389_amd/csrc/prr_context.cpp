@@ -70,7 +70,7 @@ prr::BatchArgs batch_args(const prr_batch* b) {
   a.n_seqs = b->n_seqs;
   // rows that a sequence can have: the device cuts cu_q to them
   a.total_q = b->cu_q ? (int)std::min((int64_t)b->total_q, (int64_t)b->n_seqs * b->max_q) : b->n_seqs;
-  a.max_q = b->max_q;
+  a.max_q = b->cu_q ? b->max_q : 1;
   a.max_kv = b->max_kv;
   a.table_stride = b->table_stride;
   return a;

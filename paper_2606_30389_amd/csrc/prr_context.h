@@ -56,7 +56,8 @@ struct PromptLaunch {
   float* part_ml;  // [nsplit][total_q * Hq][2] maximum (unscaled logits) and sum
   BatchArgs b;
   int num_kv_heads, group, max_pages, page_shift;
-  int tiles;   // upper bound of the row tiles of one KV head
+  int tiles;      // row tiles of one KV head (numbers: some sequences have fewer)
+  int seq_tiles;  // row tiles of every sequence, or 0: numbered by their rows
   int nsplit, part_tiles;  // parts of a row tile's keys, of so many tiles of 64 tokens
   int waves;   // of a workgroup, 32 rows each
   uint32_t magic;  // divides by the group size

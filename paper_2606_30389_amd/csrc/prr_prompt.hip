@@ -75,36 +75,31 @@ __device__ __forceinline__ float sum_halves(float v) {
 // x / G for 0 <= x < 2^28 (G <= 16): magic = ceil(2^32 / G), off by less than G / 2^32 of x; 0 stands for G = 1
 __device__ __forceinline__ int over_group(int x, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)x, magic) : x; }
 
-// The sequence and the row tile in it of tile number `tile` of the batch; false: no such tile.
-__device__ __forceinline__ bool find_tile(const PromptLaunch& a, int rows, int tile, int& s, int& local, Seq& sq) {
-  const auto tiles_of = [&](const Seq& x) { return ((x.q1 - x.q0) * a.group + rows - 1) / rows; };
-  if (a.b.n_seqs == 1) {
-    s = 0;
-    sq = seq_at(a.b, 0);
-    const int n = tiles_of(sq);
-    local = n - 1 - tile;
-    return tile < n;
-  }
-  int base = 0;
-  for (int s0 = 0; s0 < a.b.n_seqs; s0 += kWave) {
-    const int x = s0 + lane_id();
-    Seq mine = {0, 0, 0};
-    if (x < a.b.n_seqs) mine = seq_at(a.b, x);
-    const int inc = wave_inclusive_scan(tiles_of(mine));
-    const uint64_t past = __ballot(base + inc > tile);
-    if (past) {
-      const int at = __builtin_ctzll(past);
-      s = s0 + at;
-      sq.q0 = __builtin_amdgcn_readlane(mine.q0, at);
-      sq.q1 = __builtin_amdgcn_readlane(mine.q1, at);
-      sq.kv = __builtin_amdgcn_readlane(mine.kv, at);
-      // the last rows of a sequence have the most keys: they are taken first
-      local = base + __builtin_amdgcn_readlane(inc, at) - 1 - tile;
-      return true;
+// The sequence and the row tile in it of the batch's tile number `tile`; false: none.  Tiles are numbered by a
+// rule that needs no sums over the sequences.  With seq_tiles, every sequence has so many, and the last tile
+// of all sequences comes first, as it has the most keys.  Without, sequence s has the numbers from
+// floor(cu[s] G / rows) + s on: the next sequence's begin at least ceil(q_len G / rows) later.
+__device__ __forceinline__ bool find_tile(const PromptLaunch& a, int rows_log2, int tile, int& s, int& local, Seq& sq) {
+  s = 0;
+  local = tile;
+  if (a.b.n_seqs > 1 && a.seq_tiles) {
+    local = tile / a.b.n_seqs;
+    s = tile - local * a.b.n_seqs;
+  } else if (a.b.n_seqs > 1) {
+    const auto begin_of = [&](int x) { return (int)(((int64_t)a.b.cu_q[x] * a.group) >> rows_log2) + x; };
+    for (int n = a.b.n_seqs; n > 1;) {  // 64 candidates at a time
+      const int step = (n + kWave - 1) / kWave, lane = lane_id();
+      const bool ok = lane * step < n && begin_of(s + lane * step) <= tile;
+      const int at = max(__popcll(__ballot(ok)) - 1, 0) * step;
+      s += at;
+      n = min(step, n - at);
     }
-    base += __builtin_amdgcn_readlane(inc, kWave - 1);
+    local -= begin_of(s);
   }
-  return false;
+  sq = seq_at(a.b, s);
+  const int n = ((sq.q1 - sq.q0) * a.group + (1 << rows_log2) - 1) >> rows_log2;
+  local = (a.seq_tiles ? a.seq_tiles : n) - 1 - local;
+  return local >= 0 && local < n;
 }
 
 template <bool BF16, bool PAGED, int NW, bool TURNS>
@@ -121,7 +116,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
   const int h = blockIdx.x % a.num_kv_heads, part = blockIdx.y;
   int s, local;
   Seq sq;
-  if (!find_tile(a, kRows, blockIdx.x / a.num_kv_heads, s, local, sq)) return;
+  if (!find_tile(a, NW == 8 ? 8 : 7, blockIdx.x / a.num_kv_heads, s, local, sq)) return;
   const int rows = (sq.q1 - sq.q0) * G;
   const int row0 = local * kRows;
   const int first = sq.kv - (sq.q1 - sq.q0);  // position of the sequence's first new token
@@ -474,11 +469,6 @@ __global__ __launch_bounds__(256) void merge_prompt_kernel(const PromptLaunch a)
 }  // namespace
 
 void plan_prompt(PromptLaunch& a) {
-  const auto tiles_of = [&](int rows) {
-    const int64_t packed = (int64_t)a.b.total_q * a.group / rows + a.b.n_seqs;
-    const int64_t each = (int64_t)a.b.n_seqs * (((int64_t)a.b.max_q * a.group + rows - 1) / rows);
-    return min(packed, each);
-  };
   const int64_t key_tiles = max(((int64_t)a.b.max_kv + kTokens - 1) / kTokens, (int64_t)1);
   // Parts of a row tile's keys.  Fewer workgroups than CUs: as many parts, of at least eight tiles, as fill
   // the chip once (509 new of 65536 tokens, 28 / 4 heads: 460 us in four parts, 1403 in one; twice as many small
@@ -492,7 +482,12 @@ void plan_prompt(PromptLaunch& a) {
   };
   a.waves = key_tiles <= 16 ? 4 : 8;
   a.magic = a.group == 1 ? 0u : (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
-  a.tiles = (int)tiles_of(32 * a.waves);
+  const int rows = 32 * a.waves;
+  const int64_t per = ((int64_t)a.b.max_q * a.group + rows - 1) / rows, each = a.b.n_seqs * per;
+  const int64_t packed = (int64_t)a.b.total_q * a.group / rows + a.b.n_seqs;
+  const bool alike = each <= packed || !a.b.cu_q;
+  a.seq_tiles = alike ? (int)per : 0;
+  a.tiles = (int)(alike ? each : packed);
   const int64_t parts = parts_of((int64_t)a.tiles * a.num_kv_heads);
   a.part_tiles = (int)((key_tiles + parts - 1) / parts);
   a.nsplit = (int)((key_tiles + a.part_tiles - 1) / a.part_tiles);

@@ -80,6 +80,27 @@ def test_prompt_many_sequences():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("long_at", [0, 700, 1499])
+def test_prompt_one_long_among_many(long_at):
+    """1500 sequences of 0 to 6 new tokens and one of 600: tiles are numbered by rows."""
+    new = [(11 * i) % 7 for i in range(1500)]
+    new[long_at] = 600
+    kv = [n + (i % 4) * 3 for i, n in enumerate(new)]
+    run_case(new, kv, 4, 1, pad=1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 63, 64, 65, 129])
+def test_prompt_tile_numbers(n):
+    """Lengths around whole tiles of 128 and 256 rows, in both numberings (one much longer, or all alike)."""
+    new = [[31, 32, 33, 64, 0, 1, 63][i % 7] for i in range(n)]
+    kv = [x + (1100 if i == n // 2 else 2) for i, x in enumerate(new)]  # (longer than 1024: eight waves)
+    run_case(new, kv, 8, 2)
+    run_case(new + [500], kv + [500], 8, 2)
+    run_case(new, [x + 1 for x in new], 8, 2, dt="f16")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("new,kv", [([3], [5000]), ([1, 2], [3000, 4097]), ([130], [2000])])
 @pytest.mark.parametrize("hq,hkv", [(16, 1), (2, 2)])
 def test_prompt_few_rows_many_keys(new, kv, hq, hkv):
