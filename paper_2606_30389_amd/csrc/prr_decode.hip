@@ -255,7 +255,7 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
   const float l = sum_rows(st.l);
   const float norm = l > 0.0f || l != l ? exp2_hw(E4M3 ? st.yref - st.ref : 0.0f) / l : 0.0f;
   // l relative to the logit itself, not to its rounded product with the scale
-  const float exact = st.mx == kNegInf ? 0.0f : l * exp2_hw(-fmaf(st.mx, kSoftmaxScale2, -st.ref));
+  const float exact = l == 0.0f || l != l ? l : l * exp2_hw(-fmaf(st.mx, kSoftmaxScale2, -st.ref));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
     }
   }
   if (j == 0) {
-    S.m[w][n] = st.mx;
+    S.m[w][n] = l != l ? l : st.mx;  // (maxima pass over NaN: a state of NaN must not look empty)
     S.l[w][n] = exact;
   }
   __syncthreads();
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
       const int64_t at = ((int64_t)(s * a.c.num_kv_heads + h) * a.nsplit + part) * G + g;
       *reinterpret_cast<float4*>(a.part_o + at * kHeadDim + c4) = o;
       if (c4 == 0) {
-        a.part_ml[2 * at] = mx;
+        a.part_ml[2 * at] = sum != sum ? sum : mx;
         a.part_ml[2 * at + 1] = sum;
       }
     }

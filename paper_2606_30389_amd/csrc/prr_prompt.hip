@@ -372,7 +372,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
   l = sum_halves(l);
   const float inv = l != 0.0f ? 1.0f / l : 0.0f;
   // l relative to the logit itself, not to its rounded product with the scale (and the slack)
-  const float exact = mx == kNegInf ? 0.0f : l * exp2_hw(-fmaf(mx, kSoftmaxScale2, -ref));
+  const float exact = l == 0.0f || l != l ? l : l * exp2_hw(-fmaf(mx, kSoftmaxScale2, -ref));
   if (a.nsplit == 1) {
     // (the halves of a wave swap four of their eight channels, so that a store holds 16 bytes of a row)
     uint16_t* o = static_cast<uint16_t*>(a.out_o) + out_row * kHeadDim + 8 * hf;
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
               make_float4(acc[cb][i] * inv, acc[cb][i + 1] * inv, acc[cb][i + 2] * inv, acc[cb][i + 3] * inv);
     }
     if (hf == 0) {
-      a.part_ml[2 * x] = mx;
+      a.part_ml[2 * x] = l != l ? l : mx;  // (maxima pass over NaN: a state of NaN must not look empty)
       a.part_ml[2 * x + 1] = exact;
     }
   }

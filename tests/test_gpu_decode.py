@@ -197,3 +197,29 @@ def test_decode_repeats_graphs_and_streams(kind):
         torch.cuda.synchronize()
         # (a row's third sequence holds no page of its own: its lengths here stay within its table's width)
         assert all(torch.equal(x[:2], y[:2]) for x, y in zip(eager, out))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["16", "e4m3"])
+@pytest.mark.parametrize("kv", [40, 9000])
+def test_decode_nan_is_not_an_empty_state(kv, kind):
+    """A query or keys of NaN give NaN, in one part and in many; other sequences and heads are untouched."""
+    c = Case([kv, 300], 8, 2, kind=kind)
+    want = c.check()
+    c.q[0, 1] = math.nan
+    out = c.run()
+    torch.cuda.synchronize()
+    assert out[0][0, 1].isnan().all() and out[1][0, 1].isnan().all() and out[3][0, 1].isnan()
+    keep = torch.ones(2, 8, dtype=torch.bool, device=DEV)
+    keep[0, 1] = False
+    assert all(torch.equal(x[keep], y[keep]) for x, y in zip(out, want))
+    c.q[0, 1] = 1.0
+    slot = c.b.slots(1, 0, 300).to(DEV)
+    if kind == "e4m3":
+        c.cache[0].view(torch.uint8)[0].flatten(0, 1)[slot] = 0x7f
+    else:
+        c.cache[0][0].flatten(0, 1)[slot] = math.nan
+    out = c.run()
+    torch.cuda.synchronize()
+    assert out[0][1, :4].isnan().all() and out[3][1, :4].isnan().all()
+    assert all(torch.equal(x[1, 4:], y[1, 4:]) for x, y in zip(out, want))

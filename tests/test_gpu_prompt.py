@@ -210,3 +210,18 @@ def test_prompt_replayed_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip((out, m, l), want))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new,kv", [([20], [50]), ([20], [9000]), ([700], [2000])])
+def test_prompt_nan_is_not_an_empty_state(new, kv):
+    """A query of NaN gives NaN, in one part and in many; other rows are untouched."""
+    P, dims, batch, q, cache, out, m, l, ws, nbytes = run_case(new, kv, 8, 2)
+    want = [x.clone() for x in (out, m, l)]
+    q[7, 3] = math.nan
+    P.prr_prompt_attn(dims, batch, q, *cache, out, m, l, ws, nbytes)
+    torch.cuda.synchronize()
+    assert out[7, 3].isnan().all() and l[7, 3].isnan()
+    keep = torch.ones(new[0], 8, dtype=torch.bool, device=DEV)
+    keep[7, 3] = False
+    assert all(torch.equal(x[keep], y[keep]) for x, y in zip((out, m, l), want))
