@@ -100,6 +100,8 @@ class Batch:
         if len(new) != len(kv) or not len(new) or min(new) < 0 or min(kv) < 0:
             raise ValueError("new and kv: lengths of the same sequences, at least one, none negative")
         cu = np.concatenate([[0], np.cumsum(np.asarray(new, dtype=np.int64))]).astype(np.int32)
+        if page_table is not None:
+            _check_ints(page_table, "page_table", (len(new), page_table.shape[-1]))
         self._longest, self._max_kv = max(kv), max(kv) if max_kv is None else max_kv
         self.kv_len = torch.tensor(list(kv), dtype=torch.int32, device=device)
         self.page_table = page_table
@@ -133,10 +135,17 @@ def _stream_context(stream, device):
     return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream)
 
 
-def _check_rows(x, name, heads, dtype, dense):
-    if x.dtype != dtype or x.dim() != 3 or tuple(x.shape[1:]) != (heads, 128) or (dense and not x.is_contiguous()):
-        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}, strides {x.stride()}; expected {'dense ' if dense else ''}"
-                         f"{dtype} [rows][{heads}][128]")
+def _check_rows(x, name, rows, heads, dtype, dense):
+    shape = x.shape
+    if x.dtype != dtype or len(shape) != 3 or shape[0] != rows or shape[1] != heads or shape[2] != 128 or \
+            (dense and not x.is_contiguous()):
+        raise ValueError(f"{name}: {x.dtype} {tuple(shape)}, strides {x.stride()}; expected {'dense ' if dense else ''}"
+                         f"{dtype} [{rows}][{heads}][128]")
+
+
+def _check_ints(x, name, shape):
+    if x.dtype != torch.int32 or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
+        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}, strides {x.stride()}; expected dense int32 {tuple(shape)}")
 
 
 class PagedCache:
@@ -154,6 +163,8 @@ class PagedCache:
         self.k = torch.zeros(shape, dtype=torch.uint8, device=device).view(dtype) if k is None and kind == "e4m3" else \
             torch.zeros(shape, dtype=dtype, device=device) if k is None else k
         self.v = torch.zeros_like(self.k) if v is None else v
+        if any(tuple(x.shape) != shape or x.dtype.itemsize != dtype.itemsize or not x.is_contiguous() for x in (self.k, self.v)):
+            raise ValueError(f"k, v: expected dense {dtype} {shape}")
         self.k_scale = self.v_scale = None
         if kind == "e4m3":  # (exponent bytes of the rows' powers of two: 127 is 1)
             self.k_scale = torch.full(shape[:3], 127, dtype=torch.uint8, device=device)
@@ -163,16 +174,22 @@ class PagedCache:
     def _workspace(self, nbytes, stream):
         if not nbytes:
             return None
-        kept = self._ws.setdefault(L._stream(stream), [])
+        raw = torch._C._cuda_getCurrentRawStream(self.k.device.index) if stream is None else L._stream(stream)
+        kept = self._ws.setdefault(raw, [])
         if not kept or kept[-1].numel() < nbytes:
-            kept.append(torch.empty(nbytes, dtype=torch.uint8, device=self.k.device))
+            with _stream_context(stream, self.k.device):
+                kept.append(torch.empty(nbytes, dtype=torch.uint8, device=self.k.device))
         return kept[-1]
 
     def append(self, batch: Batch, q, k, v, rope: Optional[Rope] = None, positions=None, q_out=None, stream=None):
         """New tokens' keys and values into the cache, rotated; returns the rotated queries."""
-        for x, name, heads in ((q, "q", self.cfg.num_q_heads), (k, "k", self.cfg.num_kv_heads), (v, "v", self.cfg.num_kv_heads)):
+        cfg, rows = self.cfg, batch.total_q
+        for x, name, heads, dense in ((q, "q", cfg.num_q_heads, False), (k, "k", cfg.num_kv_heads, False),
+                                      (v, "v", cfg.num_kv_heads, False), (q_out, "q_out", cfg.num_q_heads, True)):
             if x is not None:
-                _check_rows(x, name, heads, self.cfg.torch_dtype, False)
+                _check_rows(x, name, rows, heads, cfg.torch_dtype, dense)
+        if positions is not None:
+            _check_ints(positions, "positions", (rows,))
         if q is not None and q_out is None:
             with _stream_context(stream, self.k.device):
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -186,36 +203,40 @@ class PagedCache:
         """Causal attention of the new tokens: (o in the 16-bit type, m, l)."""
         if self.kind != L.PRR_KV_16:
             raise ValueError("prompts attend a 16-bit cache: read() the pages back first")
-        _check_rows(q, "q", self.cfg.num_q_heads, self.cfg.torch_dtype, True)
+        _check_rows(q, "q", batch.total_q, self.cfg.num_q_heads, self.cfg.torch_dtype, True)
         nbytes = L.prr_prompt_workspace_size(self.dims, batch.native)
-        with _stream_context(stream, self.k.device):
-            if out is None:
+        if out is None:
+            with _stream_context(stream, self.k.device):
                 n, hq = q.shape[:2]
                 out = (torch.zeros_like(q), *(torch.zeros(n, hq, dtype=torch.float32, device=q.device) for _ in range(2)))
-            ws = self._workspace(nbytes, stream)
-        L.prr_prompt_attn(self.dims, batch.native, q, self.k, self.v, *out, ws, nbytes, stream)
+        L.prr_prompt_attn(self.dims, batch.native, q, self.k, self.v, *out, self._workspace(nbytes, stream), nbytes, stream)
         return out
 
     def attend(self, batch: Batch, q, pages=None, counts=None, out=None, stream=None):
         """Attention of one token per sequence over its whole cache, or over listed pages
         ([sequence][KV head][cap] and [sequence][KV head]): (o float32, o in the 16-bit type, m, l)."""
-        _check_rows(q, "q", self.cfg.num_q_heads, self.cfg.torch_dtype, True)
+        _check_rows(q, "q", batch.total_q, self.cfg.num_q_heads, self.cfg.torch_dtype, True)
         cap = 0 if pages is None else pages.shape[-1]
+        if pages is not None:
+            per_head = (batch.native.n_seqs, self.cfg.num_kv_heads)
+            _check_ints(pages, "pages", (*per_head, cap))
+            _check_ints(counts, "counts", per_head)
         nbytes = L.prr_decode_workspace_size(self.dims, batch.native, self.kind, cap)
-        with _stream_context(stream, self.k.device):
-            if out is None:
+        if out is None:
+            with _stream_context(stream, self.k.device):
                 n, hq = q.shape[:2]
                 f32 = dict(dtype=torch.float32, device=q.device)
                 out = (torch.zeros(n, hq, 128, **f32), torch.zeros_like(q), torch.zeros(n, hq, **f32), torch.zeros(n, hq, **f32))
-            ws = self._workspace(nbytes, stream)
         L.prr_decode_attn(self.dims, batch.native, q, self.kind, self.k, self.v, self.k_scale, self.v_scale, pages, counts, cap,
-                          *out, ws, nbytes, stream)
+                          *out, self._workspace(nbytes, stream), nbytes, stream)
         return out
 
     def read(self, num_tokens, page_table=None, page_begin=0, page_end=None, out=None, stream=None):
         """Pages of a sequence of an e4m3 cache in 16 bits: (k, v) [Hkv][pages][page_size][128]."""
         if page_end is None:
             page_end = -(-num_tokens // self.cfg.page_size)
+        if page_table is not None and page_table.numel() < page_end:
+            raise ValueError(f"page_table has {page_table.numel()} entries, {page_end} are read")
         if out is None:
             shape = (self.cfg.num_kv_heads, page_end - page_begin, self.cfg.page_size, 128)
             with _stream_context(stream, self.k.device):

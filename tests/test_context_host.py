@@ -226,6 +226,45 @@ def test_batches_of_the_runtime_are_checked():
     assert p.cu_q.tolist() == [0, 3, 3, 5] and p.native.max_q == 3 and p.native.total_q == 5
 
 
+def test_tensors_of_the_runtime_are_checked():
+    """Wrong shapes, types and strides are refused before any launch."""
+    import torch
+    from paper_2606_30389_amd import runtime as R
+    pc = R.PathConfig(num_q_heads=4, num_kv_heads=2, page_size=16, num_tokens=64, k_select=1)
+    c = R.PagedCache(pc, "cpu")
+    q, k = torch.zeros(5, 4, 128, dtype=torch.bfloat16), torch.zeros(5, 2, 128, dtype=torch.bfloat16)
+    table = torch.zeros(2, 4, dtype=torch.int32)
+    b = R.Batch("cpu", [3, 2], [3, 9], table)
+    for bad in (q[:4], q.half(), q[:, :2], q[..., :64], q.view(5, 512)):
+        for call in (lambda: c.append(b, bad, k, k), lambda: c.prompt(b, bad), lambda: c.append(b, q, k, k, q_out=bad)):
+            with pytest.raises(ValueError):
+                call()
+    for bad in (k[:4], k.float(), q):
+        with pytest.raises(ValueError):
+            c.append(b, q, bad, k)
+        with pytest.raises(ValueError):
+            c.append(b, q, k, bad)
+    with pytest.raises(ValueError):
+        c.append(b, q, k, k, positions=torch.zeros(4, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        c.prompt(b, torch.zeros(5, 8, 128, dtype=torch.bfloat16)[:, ::2])
+    one = R.Batch("cpu", [1, 1], [3, 9], table)
+    for pages, counts in ((torch.zeros(2, 2, 3), torch.zeros(2, 2, dtype=torch.int32)),
+                          (torch.zeros(1, 2, 3, dtype=torch.int32), torch.zeros(2, 2, dtype=torch.int32)),
+                          (torch.zeros(2, 2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))):
+        with pytest.raises(ValueError):
+            c.attend(one, q[:2], pages, counts)
+    for bad in (table[:1], table.long(), torch.zeros(4, 2, dtype=torch.int32).T):
+        with pytest.raises(ValueError):
+            R.Batch("cpu", [1, 1], [3, 9], bad)
+    with pytest.raises(ValueError):
+        R.PagedCache(pc, "cpu", kind="e4m3").prompt(b, q)
+    with pytest.raises(ValueError):
+        R.PagedCache(pc, "cpu", kind="e4m3").read(64, table[0][:3])
+    with pytest.raises(ValueError):
+        R.PagedCache(pc, "cpu", k=torch.zeros(2, 3, 16, 128, dtype=torch.bfloat16))
+
+
 # ------------------------------------------------------------------------------- frequencies
 
 @pytest.mark.parametrize("rot", [4, 64, 96, 128])
