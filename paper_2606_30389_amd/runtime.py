@@ -100,10 +100,10 @@ class Batch:
         if len(new) != len(kv) or not len(new) or min(new) < 0 or min(kv) < 0:
             raise ValueError("new and kv: lengths of the same sequences, at least one, none negative")
         cu = np.concatenate([[0], np.cumsum(np.asarray(new, dtype=np.int64))]).astype(np.int32)
-        if page_table is not None:
-            _check_ints(page_table, "page_table", (len(new), page_table.shape[-1]))
         self._longest, self._max_kv = max(kv), max(kv) if max_kv is None else max_kv
         self.kv_len = torch.tensor(list(kv), dtype=torch.int32, device=device)
+        if page_table is not None:
+            _check(page_table, "page_table", (len(new), page_table.shape[-1]), torch.int32, self.kv_len.device)
         self.page_table = page_table
         # one new token each: rows are sequences
         self.cu_q = None if all(n == 1 for n in new) else torch.from_numpy(cu).to(device)
@@ -135,17 +135,11 @@ def _stream_context(stream, device):
     return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream)
 
 
-def _check_rows(x, name, rows, heads, dtype, dense):
-    shape = x.shape
-    if x.dtype != dtype or len(shape) != 3 or shape[0] != rows or shape[1] != heads or shape[2] != 128 or \
-            (dense and not x.is_contiguous()):
-        raise ValueError(f"{name}: {x.dtype} {tuple(shape)}, strides {x.stride()}; expected {'dense ' if dense else ''}"
-                         f"{dtype} [{rows}][{heads}][128]")
-
-
-def _check_ints(x, name, shape):
-    if x.dtype != torch.int32 or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
-        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}, strides {x.stride()}; expected dense int32 {tuple(shape)}")
+def _check(x, name, shape, dtype, device, dense=True):
+    """x has the shape, type and device that the kernels take for granted."""
+    if x.dtype != dtype or x.shape != shape or x.device != device or (dense and not x.is_contiguous()):
+        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}; expected "
+                         f"{'dense ' if dense else ''}{dtype} {tuple(shape)} on {device}")
 
 
 class PagedCache:
@@ -163,13 +157,22 @@ class PagedCache:
         self.k = torch.zeros(shape, dtype=torch.uint8, device=device).view(dtype) if k is None and kind == "e4m3" else \
             torch.zeros(shape, dtype=dtype, device=device) if k is None else k
         self.v = torch.zeros_like(self.k) if v is None else v
-        if any(tuple(x.shape) != shape or x.dtype.itemsize != dtype.itemsize or not x.is_contiguous() for x in (self.k, self.v)):
-            raise ValueError(f"k, v: expected dense {dtype} {shape}")
+        for x, name in ((self.k, "k"), (self.v, "v")):
+            _check(x, name, shape, dtype, self.k.device)
+        if self.k.device.type != torch.device(device).type:
+            raise ValueError(f"k: on {self.k.device}, expected on {device}")
         self.k_scale = self.v_scale = None
         if kind == "e4m3":  # (exponent bytes of the rows' powers of two: 127 is 1)
-            self.k_scale = torch.full(shape[:3], 127, dtype=torch.uint8, device=device)
-            self.v_scale = torch.full(shape[:3], 127, dtype=torch.uint8, device=device)
+            self.k_scale = torch.full(shape[:3], 127, dtype=torch.uint8, device=self.k.device)
+            self.v_scale = torch.full(shape[:3], 127, dtype=torch.uint8, device=self.k.device)
         self._ws = {}
+
+    def _check_batch(self, batch, q):
+        """The device of the batch's lengths; the queries of a call that attends."""
+        if batch.kv_len.device != self.k.device:
+            raise ValueError(f"batch: on {batch.kv_len.device}, expected on {self.k.device}")
+        if q is not None:
+            _check(q, "q", (batch.total_q, self.cfg.num_q_heads, 128), self.cfg.torch_dtype, self.k.device)
 
     def _workspace(self, nbytes, stream):
         if not nbytes:
@@ -187,9 +190,12 @@ class PagedCache:
         for x, name, heads, dense in ((q, "q", cfg.num_q_heads, False), (k, "k", cfg.num_kv_heads, False),
                                       (v, "v", cfg.num_kv_heads, False), (q_out, "q_out", cfg.num_q_heads, True)):
             if x is not None:
-                _check_rows(x, name, rows, heads, cfg.torch_dtype, dense)
+                _check(x, name, (rows, heads, 128), cfg.torch_dtype, self.k.device, dense)
+        self._check_batch(batch, None)
         if positions is not None:
-            _check_ints(positions, "positions", (rows,))
+            _check(positions, "positions", (rows,), torch.int32, self.k.device)
+        if rope is not None and rope.freqs.device != self.k.device:
+            raise ValueError(f"rope: on {rope.freqs.device}, expected on {self.k.device}")
         if q is not None and q_out is None:
             with _stream_context(stream, self.k.device):
                 q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -203,30 +209,37 @@ class PagedCache:
         """Causal attention of the new tokens: (o in the 16-bit type, m, l)."""
         if self.kind != L.PRR_KV_16:
             raise ValueError("prompts attend a 16-bit cache: read() the pages back first")
-        _check_rows(q, "q", batch.total_q, self.cfg.num_q_heads, self.cfg.torch_dtype, True)
+        self._check_batch(batch, q)
         nbytes = L.prr_prompt_workspace_size(self.dims, batch.native)
         if out is None:
             with _stream_context(stream, self.k.device):
                 n, hq = q.shape[:2]
                 out = (torch.zeros_like(q), *(torch.zeros(n, hq, dtype=torch.float32, device=q.device) for _ in range(2)))
+        else:
+            for x, name, ref in zip(out, ("o", "m", "l"), (q.shape, q.shape[:2], q.shape[:2]), strict=True):
+                _check(x, name, ref, q.dtype if name == "o" else torch.float32, self.k.device)
         L.prr_prompt_attn(self.dims, batch.native, q, self.k, self.v, *out, self._workspace(nbytes, stream), nbytes, stream)
         return out
 
     def attend(self, batch: Batch, q, pages=None, counts=None, out=None, stream=None):
         """Attention of one token per sequence over its whole cache, or over listed pages
         ([sequence][KV head][cap] and [sequence][KV head]): (o float32, o in the 16-bit type, m, l)."""
-        _check_rows(q, "q", batch.total_q, self.cfg.num_q_heads, self.cfg.torch_dtype, True)
+        self._check_batch(batch, q)
         cap = 0 if pages is None else pages.shape[-1]
         if pages is not None:
             per_head = (batch.native.n_seqs, self.cfg.num_kv_heads)
-            _check_ints(pages, "pages", (*per_head, cap))
-            _check_ints(counts, "counts", per_head)
+            _check(pages, "pages", (*per_head, cap), torch.int32, self.k.device)
+            _check(counts, "counts", per_head, torch.int32, self.k.device)
         nbytes = L.prr_decode_workspace_size(self.dims, batch.native, self.kind, cap)
         if out is None:
             with _stream_context(stream, self.k.device):
                 n, hq = q.shape[:2]
                 f32 = dict(dtype=torch.float32, device=q.device)
                 out = (torch.zeros(n, hq, 128, **f32), torch.zeros_like(q), torch.zeros(n, hq, **f32), torch.zeros(n, hq, **f32))
+        else:
+            for x, name, ref in zip(out, ("o32", "o", "m", "l"), (q.shape, q.shape, q.shape[:2], q.shape[:2]), strict=True):
+                if x is not None:
+                    _check(x, name, ref, q.dtype if name == "o" else torch.float32, self.k.device)
         L.prr_decode_attn(self.dims, batch.native, q, self.kind, self.k, self.v, self.k_scale, self.v_scale, pages, counts, cap,
                           *out, self._workspace(nbytes, stream), nbytes, stream)
         return out
@@ -235,12 +248,17 @@ class PagedCache:
         """Pages of a sequence of an e4m3 cache in 16 bits: (k, v) [Hkv][pages][page_size][128]."""
         if page_end is None:
             page_end = -(-num_tokens // self.cfg.page_size)
-        if page_table is not None and page_table.numel() < page_end:
-            raise ValueError(f"page_table has {page_table.numel()} entries, {page_end} are read")
+        if page_table is not None:
+            _check(page_table, "page_table", (max(page_end, page_table.numel()),), torch.int32, self.k.device)
+        shape = (self.cfg.num_kv_heads, page_end - page_begin, self.cfg.page_size, 128)
         if out is None:
-            shape = (self.cfg.num_kv_heads, page_end - page_begin, self.cfg.page_size, 128)
+            if page_begin < 0 or page_end < page_begin:
+                raise ValueError(f"pages {page_begin} to {page_end}")
             with _stream_context(stream, self.k.device):
                 out = tuple(torch.zeros(shape, dtype=self.cfg.torch_dtype, device=self.k.device) for _ in range(2))
+        else:
+            for x, name in zip(out, ("k", "v"), strict=True):
+                _check(x, name, shape, self.cfg.torch_dtype, self.k.device)
         L.prr_cache_read(self.dims, self.k, self.v, self.k_scale, self.v_scale, page_table, num_tokens, page_begin, page_end,
                          *out, stream)
         return out

@@ -263,6 +263,38 @@ def test_tensors_of_the_runtime_are_checked():
         R.PagedCache(pc, "cpu", kind="e4m3").read(64, table[0][:3])
     with pytest.raises(ValueError):
         R.PagedCache(pc, "cpu", k=torch.zeros(2, 3, 16, 128, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        R.PagedCache(pc, "cpu", k=torch.zeros(2, 4, 16, 128, dtype=torch.float16))
+
+
+def test_outputs_and_devices_of_the_runtime_are_checked():
+    """Outputs that are given have the size of what is written; nothing lies on another device."""
+    import torch
+    from paper_2606_30389_amd import runtime as R
+    pc = R.PathConfig(num_q_heads=4, num_kv_heads=2, page_size=16, num_tokens=64, k_select=1)
+    c, e = R.PagedCache(pc, "cpu"), R.PagedCache(pc, "cpu", kind="e4m3")
+    q, ml = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(2, 4)
+    b, elsewhere = R.Batch("cpu", [1, 1], [3, 9]), R.Batch("meta", [1, 1], [3, 9])
+    for out in ((q[:1], ml, ml), (q.float(), ml, ml), (q, ml[:1], ml), (q, ml, ml.double()), (q, ml)):
+        with pytest.raises(ValueError):
+            c.prompt(b, q, out=out)
+    for out in ((q, q, ml, ml), (q.float(), q.float(), ml, ml), (q.float(), q, ml[:, :2], ml), (q.float(), q, ml, ml[:1]),
+                (q.float()[:1], None, ml, ml), (q.float(), q, ml)):
+        with pytest.raises(ValueError):
+            c.attend(b, q, out=out)
+    for call in (lambda: c.prompt(elsewhere, q), lambda: c.attend(elsewhere, q), lambda: c.append(elsewhere, None, q[:, :2], q[:, :2]),
+                 lambda: c.attend(b, q.to("meta")), lambda: c.append(b, q, q[:, :2], q[:, :2], R.Rope("meta")),
+                 lambda: R.Batch("cpu", [1], [3], torch.zeros(1, 4, dtype=torch.int32, device="meta"))):
+        with pytest.raises(ValueError):
+            call()
+    pages = torch.zeros(2, 4, 16, 128, dtype=torch.bfloat16)
+    for out in ((pages[:, :3], pages), (pages, pages.float()), (pages,), (pages, pages.to("meta"))):
+        with pytest.raises(ValueError):
+            e.read(64, out=out)
+    for args in (dict(page_begin=3, page_end=2), dict(page_begin=-1), dict(page_table=torch.zeros(4, dtype=torch.int64)),
+                 dict(page_table=torch.zeros(8, dtype=torch.int32)[::2])):
+        with pytest.raises(ValueError):
+            e.read(64, **args)
 
 
 # ------------------------------------------------------------------------------- frequencies
