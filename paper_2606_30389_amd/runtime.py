@@ -137,6 +137,8 @@ def _stream_context(stream, device):
 
 def _check(x, name, shape, dtype, device, dense=True):
     """x has the shape, type and device that the kernels take for granted."""
+    if x is None:
+        raise ValueError(f"{name} is missing")
     if x.dtype != dtype or x.shape != shape or x.device != device or (dense and not x.is_contiguous()):
         raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}, strides {x.stride()}, on {x.device}; expected "
                          f"{'dense ' if dense else ''}{dtype} {tuple(shape)} on {device}")
@@ -206,7 +208,7 @@ class PagedCache:
         return q_out
 
     def prompt(self, batch: Batch, q, out=None, stream=None):
-        """Causal attention of the new tokens: (o in the 16-bit type, m, l)."""
+        """Causal attention of the new tokens: (o in the 16-bit type, m, l); in `out`, m and l may both be None."""
         if self.kind != L.PRR_KV_16:
             raise ValueError("prompts attend a 16-bit cache: read() the pages back first")
         self._check_batch(batch, q)
@@ -217,13 +219,16 @@ class PagedCache:
                 out = (torch.zeros_like(q), *(torch.zeros(n, hq, dtype=torch.float32, device=q.device) for _ in range(2)))
         else:
             for x, name, ref in zip(out, ("o", "m", "l"), (q.shape, q.shape[:2], q.shape[:2]), strict=True):
+                if x is None and name != "o":
+                    continue  # (the call itself refuses one of m and l alone)
                 _check(x, name, ref, q.dtype if name == "o" else torch.float32, self.k.device)
         L.prr_prompt_attn(self.dims, batch.native, q, self.k, self.v, *out, self._workspace(nbytes, stream), nbytes, stream)
         return out
 
     def attend(self, batch: Batch, q, pages=None, counts=None, out=None, stream=None):
         """Attention of one token per sequence over its whole cache, or over listed pages
-        ([sequence][KV head][cap] and [sequence][KV head]): (o float32, o in the 16-bit type, m, l)."""
+        ([sequence][KV head][cap] and [sequence][KV head]): (o float32, o in the 16-bit type, m, l);
+        in `out`, the 16-bit o may be None."""
         self._check_batch(batch, q)
         cap = 0 if pages is None else pages.shape[-1]
         if pages is not None:
@@ -238,7 +243,7 @@ class PagedCache:
                 out = (torch.zeros(n, hq, 128, **f32), torch.zeros_like(q), torch.zeros(n, hq, **f32), torch.zeros(n, hq, **f32))
         else:
             for x, name, ref in zip(out, ("o32", "o", "m", "l"), (q.shape, q.shape, q.shape[:2], q.shape[:2]), strict=True):
-                if x is not None:
+                if x is not None or name != "o":
                     _check(x, name, ref, q.dtype if name == "o" else torch.float32, self.k.device)
         L.prr_decode_attn(self.dims, batch.native, q, self.kind, self.k, self.v, self.k_scale, self.v_scale, pages, counts, cap,
                           *out, self._workspace(nbytes, stream), nbytes, stream)

@@ -275,11 +275,11 @@ def test_outputs_and_devices_of_the_runtime_are_checked():
     c, e = R.PagedCache(pc, "cpu"), R.PagedCache(pc, "cpu", kind="e4m3")
     q, ml = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(2, 4)
     b, elsewhere = R.Batch("cpu", [1, 1], [3, 9]), R.Batch("meta", [1, 1], [3, 9])
-    for out in ((q[:1], ml, ml), (q.float(), ml, ml), (q, ml[:1], ml), (q, ml, ml.double()), (q, ml)):
+    for out in ((q[:1], ml, ml), (q.float(), ml, ml), (q, ml[:1], ml), (q, ml, ml.double()), (q, ml), (None, ml, ml)):
         with pytest.raises(ValueError):
             c.prompt(b, q, out=out)
     for out in ((q, q, ml, ml), (q.float(), q.float(), ml, ml), (q.float(), q, ml[:, :2], ml), (q.float(), q, ml, ml[:1]),
-                (q.float()[:1], None, ml, ml), (q.float(), q, ml)):
+                (q.float()[:1], None, ml, ml), (q.float(), q, ml), (None, q, ml, ml), (q.float(), q, None, ml)):
         with pytest.raises(ValueError):
             c.attend(b, q, out=out)
     for call in (lambda: c.prompt(elsewhere, q), lambda: c.attend(elsewhere, q), lambda: c.append(elsewhere, None, q[:, :2], q[:, :2]),

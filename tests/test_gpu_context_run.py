@@ -223,3 +223,26 @@ def test_two_streams_at_once():
     p = cache.prompt(prompt, q, stream=streams[0].cuda_stream)
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(p, want[0]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,new", [(40, 3), (5000, 20)])
+def test_outputs_left_out(tokens, new):
+    """Prompts without m and l, single tokens without the 16-bit output (one part and several): the others do not change."""
+    from paper_2606_30389_amd import _lib as L
+    from paper_2606_30389_amd import runtime as R
+    pc = R.PathConfig(num_q_heads=8, num_kv_heads=2, page_size=16, num_tokens=tokens, k_select=1)
+    cache = R.PagedCache(pc, DEV)
+    g = torch.Generator(device=DEV).manual_seed(9)
+    cache.k.copy_(torch.randn(cache.k.shape, generator=g, device=DEV))
+    cache.v.copy_(torch.randn(cache.v.shape, generator=g, device=DEV))
+    q = torch.randn(new, 8, S.D, generator=g, device=DEV).to(torch.bfloat16)
+    prompt, one = R.Batch(DEV, [new], [tokens]), R.Batch(DEV, [1], [tokens])
+    o, m, l = cache.prompt(prompt, q)
+    got = cache.prompt(prompt, q, out=(torch.full_like(o, 7), None, None))
+    assert torch.equal(got[0], o)
+    o32, o16, m1, l1 = cache.attend(one, q[:1])
+    got = cache.attend(one, q[:1], out=(torch.full_like(o32, 7), None, torch.full_like(m1, 7), torch.full_like(l1, 7)))
+    assert torch.equal(got[0], o32) and torch.equal(got[2], m1) and torch.equal(got[3], l1)
+    with pytest.raises(L.PrrError):
+        cache.prompt(prompt, q, out=(torch.empty_like(o), torch.empty_like(m), None))
