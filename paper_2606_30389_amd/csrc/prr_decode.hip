@@ -19,12 +19,15 @@ namespace {
 // row to one lane, a load each 16: 271 us where this takes 250).
 //
 // An e4m3 cache: codes are exact in either 16-bit type.  q.code is scaled by the key's power of two
-// in float32.  The value's power of two 2^ev joins the weight, p 2^ev = 2^(x + ev - y), y the largest
-// x + ev so far (x the logit in powers of two): every weight that counts is near 1, whatever the
-// scales, and the product runs in float16, whose two-term weights carry 22 bits.
+// in float32.  The value's power of two 2^ev joins the weight, exactly: p 2^(ev - top + kHeadroom), top
+// the largest ev so far.  A large scale says nothing about a row's other channels, so the weights of rows
+// with far smaller scales have to keep their bits: the product runs in bfloat16, whose three-term weights
+// have float32's bits and range, and weights up to 2^kHeadroom leave the lower 2^-126 to the others.
 constexpr int NW = 8;  // waves of a workgroup
 constexpr int kTile = 16;
 constexpr float kNoRef = -3e38f;  // nothing seen yet: 2^(kNoRef - anything later) = 0
+// (2^30 tokens of codes up to 448 stay below 2^(30 + 9 + 88) = 2^127)
+constexpr int kHeadroom = 88;
 
 template <bool E4M3>
 struct TileData {
@@ -72,11 +75,12 @@ __device__ __forceinline__ void load_tile(const CacheArgs& c, int64_t row0, int 
 }
 
 // A wave's running state: per lane the head n = lane % 16.  mx the largest logit (unscaled q.k), ref
-// the exponent (powers of two) that l is relative to, yref the one of acc (E4M3; else ref), l this
-// lane's part of the sum.
+// the exponent (powers of two) that l and acc are relative to, l this lane's part of the sum; E4M3: top
+// the largest scale byte of the values, acc relative to 2^(top - 127 - kHeadroom) too.
 struct WaveState {
   f32x4_t acc[8];
-  float mx, ref, yref, l;
+  float mx, ref, l;
+  int top;
 };
 
 template <bool BF16, bool E4M3>
@@ -95,49 +99,52 @@ __device__ __forceinline__ void attend_tile(const TileData<E4M3>& d, const u32x4
       s = mfma16<BF16>(d.k[x], qf[x], s);
     }
   }
-  float y[4], top = kNegInf, ytop = kNegInf;
+  float top = kNegInf;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const bool live = 4 * j + i < valid;
     if constexpr (E4M3) s[i] *= __uint_as_float(((d.ks >> (8 * i)) & 0xffu) << 23);
     s[i] = live ? s[i] : kNegInf;
     top = fmaxf(top, s[i]);
-    if constexpr (E4M3) {
-      y[i] = fmaf(s[i], kSoftmaxScale2, (float)(int)((d.vs >> (8 * i)) & 0xffu) - 127.0f);
-      ytop = fmaxf(ytop, y[i]);
-    }
   }
   st.mx = fmaxf(st.mx, max_rows(top));
   const float ref = st.mx == kNegInf ? st.ref : st.mx * kSoftmaxScale2;
-  st.l *= exp2_hw(st.ref - ref);
-  float yref = ref;
-  if constexpr (E4M3) {
-    ytop = fmaxf(st.yref, max_rows(ytop));
-    yref = ytop == kNegInf ? st.yref : ytop;
-  }
-  if (__any(yref != st.yref)) {
-    const float alpha = exp2_hw(st.yref - yref);
+  const float alpha = exp2_hw(st.ref - ref);
+  st.l *= alpha;
+  if (__any(ref != st.ref)) {
 #pragma unroll
     for (int cb = 0; cb < 8; ++cb) st.acc[cb] *= alpha;
   }
   st.ref = ref;
-  st.yref = yref;
+  if constexpr (E4M3) {
+    int vtop = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vtop = max(vtop, 4 * j + i < valid ? (int)((d.vs >> (8 * i)) & 0xffu) : 0);
+    if (__any(vtop > st.top)) {
+      const int next = max(st.top, (int)max_rows((float)vtop));
+#pragma unroll
+      for (int cb = 0; cb < 8; ++cb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.acc[cb][i] = ldexpf(st.acc[cb][i], st.top - next);
+      st.top = next;
+    }
+  }
   float w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float p = exp2_hw(fmaf(s[i], kSoftmaxScale2, -ref));
     st.l += p;
-    w[i] = E4M3 ? exp2_hw(y[i] - yref) : p;
+    w[i] = E4M3 ? ldexpf(p, (int)((d.vs >> (8 * i)) & 0xffu) - st.top + kHeadroom) : p;
   }
   if constexpr (E4M3) {
     u32x4_t v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      v[i] = u32x4_t{unpack_codes<false, false>(d.v[i][0], 1.0f), unpack_codes<false, true>(d.v[i][0], 1.0f),
-                     unpack_codes<false, false>(d.v[i][1], 1.0f), unpack_codes<false, true>(d.v[i][1], 1.0f)};
-    pv_tile<false>(st.acc, v, w);
+      v[i] = u32x4_t{unpack_codes<true, false>(d.v[i][0], 1.0f), unpack_codes<true, true>(d.v[i][0], 1.0f),
+                     unpack_codes<true, false>(d.v[i][1], 1.0f), unpack_codes<true, true>(d.v[i][1], 1.0f)};
+    pv_tile<true, 3>(st.acc, v, w);
   } else {
-    pv_tile<BF16, BF16 ? 3 : 2>(st.acc, d.v, w);  // (two bfloat16 terms: an error of 2e-6 where float32 has 1e-6)
+    pv_tile<BF16, BF16 ? 3 : 2>(st.acc, d.v, w);
   }
 }
 
@@ -193,8 +200,9 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) st.acc[cb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   st.mx = kNegInf;
-  st.ref = st.yref = kNoRef;
+  st.ref = kNoRef;
   st.l = 0.0f;
+  st.top = 0;
 
   const int sh = a.c.page_shift - 4;  // log2 of the tiles of a page
   const int64_t head_row = (int64_t)h * a.c.max_pages * a.c.page_size;
@@ -251,9 +259,16 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
     }
   }
 
-  // the wave's state, normalised: o = acc 2^(yref - ref) / l
+  // the wave's state, normalised
   const float l = sum_rows(st.l);
-  const float norm = l > 0.0f || l != l ? exp2_hw(E4M3 ? st.yref - st.ref : 0.0f) / l : 0.0f;
+  const float norm = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  if constexpr (E4M3) {
+    const int by = st.top - 127 - kHeadroom;
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.acc[cb][i] = ldexpf(st.acc[cb][i], by);
+  }
   // l relative to the logit itself, not to its rounded product with the scale
   const float exact = l == 0.0f || l != l ? l : l * exp2_hw(-fmaf(st.mx, kSoftmaxScale2, -st.ref));
 #pragma unroll

@@ -287,36 +287,49 @@ constexpr uint32_t kFlagSpinTimeout = 2u;
 // lo = rne(p - hi).  bfloat16 terms carry p to about 2^-17 relative; float16 terms to
 // 2^-22 relative or 2^-25 absolute (lo is subnormal below 2^-14), far inside the
 // tolerance of the outputs.  Two MFMAs replace the four fp32 16x16x4 MFMAs that a float32
-// weight operand needs, at an eighth of their issue cycles.  TERMS = 3 adds a third term, the
-// rest of the first two: bfloat16 weights to 2^-25.
+// weight operand needs, at an eighth of their issue cycles.  TERMS = 3 (bfloat16) cuts a weight's
+// 24 bits into three terms of eight, without any rounding, for two 16x16x32 MFMAs (the rows twice
+// against the first two terms, then against the third).
 template <bool BF16, int TERMS = 2>
 __device__ __forceinline__ void pv_tile(f32x4_t (&acc)[8], const u32x4_t (&v)[4], const float (&p)[4]) {
-  uint32_t hi[4], lo[4], rest[4];
+  static_assert(TERMS == 2 || (TERMS == 3 && BF16), "float16 weights have two terms");
+  uint32_t hi[4], lo[4];
+  [[maybe_unused]] uint32_t rest[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    hi[i] = f2h_rne<BF16>(p[i]);
-    lo[i] = f2h_rne<BF16>(p[i] - h2f<BF16>(hi[i]));
-    if constexpr (TERMS == 3) rest[i] = f2h_rne<BF16>((p[i] - h2f<BF16>(hi[i])) - h2f<BF16>(lo[i]));
+    if constexpr (TERMS == 3) {
+      const float x = p[i] - __uint_as_float(__float_as_uint(p[i]) & 0xffff0000u);
+      hi[i] = __float_as_uint(p[i]) >> 16;
+      lo[i] = __float_as_uint(x) >> 16;
+      rest[i] = __float_as_uint(x - __uint_as_float(__float_as_uint(x) & 0xffff0000u)) >> 16;
+    } else {
+      hi[i] = f2h_rne<BF16>(p[i]);
+      lo[i] = f2h_rne<BF16>(p[i] - h2f<BF16>(hi[i]));
+    }
   }
   const s16x4_t bh =
       __builtin_bit_cast(s16x4_t, (uint64_t)(hi[0] | (hi[1] << 16)) | ((uint64_t)(hi[2] | (hi[3] << 16)) << 32));
   const s16x4_t bl =
       __builtin_bit_cast(s16x4_t, (uint64_t)(lo[0] | (lo[1] << 16)) | ((uint64_t)(lo[2] | (lo[3] << 16)) << 32));
-  [[maybe_unused]] s16x4_t br;
-  if constexpr (TERMS == 3)
-    br = __builtin_bit_cast(s16x4_t, (uint64_t)(rest[0] | (rest[1] << 16)) | ((uint64_t)(rest[2] | (rest[3] << 16)) << 32));
+  [[maybe_unused]] bf16x8_t b01, b2;
+  if constexpr (TERMS == 3) {
+    b01 = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(bh, bl, 0, 1, 2, 3, 4, 5, 6, 7));
+    b2 = __builtin_bit_cast(bf16x8_t, u32x4_t{rest[0] | (rest[1] << 16), rest[2] | (rest[3] << 16), 0u, 0u});
+  }
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) {
     const int w = cb >> 1, sh = (cb & 1) * 16;
     const uint32_t a0 = ((v[0][w] >> sh) & 0xffffu) | (((v[1][w] >> sh) & 0xffffu) << 16);
     const uint32_t a1 = ((v[2][w] >> sh) & 0xffffu) | (((v[3][w] >> sh) & 0xffffu) << 16);
     const s16x4_t va = __builtin_bit_cast(s16x4_t, (uint64_t)a0 | ((uint64_t)a1 << 32));
-    if constexpr (BF16) {
+    if constexpr (TERMS == 3) {
+      const bf16x8_t twice = __builtin_bit_cast(bf16x8_t, u32x4_t{a0, a1, a0, a1});
+      acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(twice, b01, acc[cb], 0, 0, 0);
+      acc[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(twice, b2, acc[cb], 0, 0, 0);
+    } else if constexpr (BF16) {
       acc[cb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(va, bh, acc[cb], 0, 0, 0);
       acc[cb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(va, bl, acc[cb], 0, 0, 0);
-      if constexpr (TERMS == 3) acc[cb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(va, br, acc[cb], 0, 0, 0);
     } else {
-      static_assert(TERMS == 2, "float16 weights have two terms");
       typedef __attribute__((ext_vector_type(4))) _Float16 f16x4_t;
       acc[cb] = __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4_t, va), __builtin_bit_cast(f16x4_t, bh),
                                                       acc[cb], 0, 0, 0);

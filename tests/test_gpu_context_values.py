@@ -1,0 +1,94 @@
+"""Attention over caches whose values lie far apart: rows that one channel or a scale makes large, keys that outweigh all
+others, infinities.  Every channel is held to its own bound: what is large in one channel excuses nothing in
+another."""
+import math
+
+import pytest
+import torch
+
+from tests import context_support as S
+
+DEV = "cuda:0"
+DT = {"bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def decode(cache, scale, q, kv, dt):
+    """prr_decode_attn of one sequence of kv tokens over an identity table: o32, o, m, l."""
+    import paper_2606_30389_amd as P
+    hq, hkv, pool, page = q.shape[1], *cache[0].shape[:3]
+    dims = P.make_dims(hq, hkv, page, pool, P.PRR_BF16 if dt == "bf16" else P.PRR_F16)
+    kind = P.PRR_KV_16 if scale[0] is None else P.PRR_KV_E4M3
+    lens = torch.tensor([kv], dtype=torch.int32, device=DEV)
+    batch = P.make_batch(1, 1, 1, kv, None, lens)
+    nbytes = P.prr_decode_workspace_size(dims, batch, kind)
+    ws = torch.full((max(nbytes, 256),), 0xff, dtype=torch.uint8, device=DEV)
+    out = [torch.empty(1, hq, S.D, device=DEV), torch.empty(1, hq, S.D, dtype=DT[dt], device=DEV), torch.empty(1, hq, device=DEV),
+           torch.empty(1, hq, device=DEV)]
+    P.prr_decode_attn(dims, batch, q, kind, *cache, *scale, None, None, 0, *out, ws, nbytes)
+    torch.cuda.synchronize()
+    return out
+
+
+def check(out, q, k, v, weight_err, floor=0.0, dt="bf16", what=""):
+    """k, v [Hkv][kv][128] in 64 bits; floor [Hq][128] or a number."""
+    hkv = k.shape[0]
+    G = q.shape[1] // hkv
+    for h in range(hkv):
+        heads = slice(h * G, (h + 1) * G)
+        o, m, l, a, mag = S.attend64(q[0, heads].double(), k[h], v[h])
+        fl = floor[heads] if torch.is_tensor(floor) else floor
+        got = [x[0, heads].double() for x in out]
+        S.check_state(got[0], got[2], got[3], o, m, l, a, mag, weight_err, 2.0 ** -22, k.shape[1], fl, (what, h))
+        eps = S.half_step(DT[dt])
+        # (beyond the 16-bit type's largest number and half a step more, rounding gives infinity)
+        far = o.abs() > torch.finfo(DT[dt]).max * (1 + eps)
+        assert torch.equal(got[1][far], o[far].sign() * math.inf), what
+        o, got[1] = o.masked_fill(far, 0.0), got[1].masked_fill(far, 0.0)
+        S.check_state(got[1], got[2], got[3], o, m, l, a, mag, weight_err + eps, eps, k.shape[1],
+                      fl + (2.0 ** -25 if dt == "f16" else 0.0), (what, h))
+
+
+def e4m3_rows(code, scale, kv):
+    """The numbers of an e4m3 cache's first kv rows (identity table)."""
+    p = torch.exp2(scale.flatten(1, 2)[:, :kv].double() - 127)
+    return code.view(torch.float8_e4m3fn).flatten(1, 2)[:, :kv].double() * p[..., None]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt,outlier", [("bf16", 1e4), ("bf16", 1e6), ("bf16", 3e38), ("bf16", math.inf), ("f16", 6e4), ("f16", -math.inf)])
+@pytest.mark.parametrize("kv,at", [(16, 5), (700, 0), (700, 699), (4096, 2000), (20011, 3)])
+def test_e4m3_row_with_one_large_channel(kv, at, dt, outlier):
+    """One row's value is far larger in channel 0 than anything else: the other channels keep their accuracy.
+    Weights are three bfloat16 terms."""
+    from paper_2606_30389_amd import runtime as R
+    pc = R.PathConfig(num_q_heads=8, num_kv_heads=2, page_size=16, num_tokens=kv, k_select=1, dtype=dt)
+    cache = R.PagedCache(pc, DEV, kind="e4m3")
+    g = torch.Generator(device=DEV).manual_seed(kv + at)
+    k, v = (torch.randn(kv, 2, S.D, generator=g, device=DEV).to(DT[dt]) for _ in range(2))
+    v[at, :, 0] = outlier
+    q = (1.5 * torch.randn(1, 8, S.D, generator=g, device=DEV)).to(DT[dt])
+    cache.append(R.Batch(DEV, [kv], [kv]), None, k, v)
+    codes, scales = (cache.k.view(torch.uint8), cache.v.view(torch.uint8)), (cache.k_scale, cache.v_scale)
+    out = decode(codes, scales, q, kv, dt)
+    check(out, q, e4m3_rows(codes[0], scales[0], kv), e4m3_rows(codes[1], scales[1], kv), 2.0 ** -24, 2.0 ** -126, dt, outlier)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("large,small", [(254, 120), (200, 20), (150, 149), (60, 1), (1, 1)])
+@pytest.mark.parametrize("kv", [16, 1000])
+def test_e4m3_scales_of_rows_that_are_empty_where_it_matters(kv, large, small, dt):
+    """Rows with a large scale byte hold zeros (every third row) or one number in channel 0 (one row): the other rows
+    decide every other channel."""
+    g = torch.Generator(device=DEV).manual_seed(kv + large)
+    pages = -(-kv // 16)
+    codes = [(40 * torch.randn(2, pages, 16, S.D, generator=g, device=DEV)).to(torch.float8_e4m3fn).view(torch.uint8) for _ in range(2)]
+    scales = [torch.full((2, pages, 16), b, dtype=torch.uint8, device=DEV) for b in (120, small)]
+    v, s = codes[1].flatten(1, 2), scales[1].flatten(1, 2)
+    v[:, 1::3] = 0
+    s[:, 1::3] = large
+    v[:, 4, 0] = 0x38  # 1.0
+    q = torch.randn(1, 8, S.D, generator=g, device=DEV).to(DT[dt])
+    out = decode(codes, scales, q, kv, dt)
+    # (numbers below 2^-126 are of no account)
+    check(out, q, e4m3_rows(codes[0], scales[0], kv), e4m3_rows(codes[1], scales[1], kv), 2.0 ** -24, 2.0 ** -125, dt, (large, small))
