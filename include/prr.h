@@ -388,7 +388,7 @@ prr_status prr_prompt_attn(const prr_dims* dims, const prr_batch* batch, const v
  *   out_o32      device [total_q][Hq][128] float32 out, out_o the same in dtype, out_m, out_l
  *                [total_q][Hq] float32 out; out_o may be NULL
  * Every channel is summed in float32 accuracy by itself, whatever the scales of the rows (E4M3: down to 2^-190 of
- * the largest value scale).  List and table entries out of range are skipped.  The result does not depend on how the work is
+ * the largest value scale; a float16 cache's weights down to 2^-39 of the largest among 16 neighbouring tokens).  List and table entries out of range are skipped.  The result does not depend on how the work is
  * split but for rounding; the same call gives the same bits.  Workspace: as for prr_prompt_attn,
  * prr_decode_workspace_size bytes (cap 0 = no lists). */
 size_t prr_decode_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t kv_kind, int32_t cap);

@@ -18,6 +18,11 @@ namespace {
 // pieces go to the four lanes of a load instruction in order, 64 bytes of a row at a time (64 bytes of a
 // row to one lane, a load each 16: 271 us where this takes 250).
 //
+// Weights: bfloat16 ones are three terms, all of float32's bits.  float16 ones are two, 22 bits, of numbers that
+// a power of two per head and tile lifts to the top of float16's range: what is 2^-17 below the largest weight
+// of its 16 tokens loses bits (2^-39 of it is the step), never what is below another tile's.  (Relative to
+// the largest weight of all, 17 nats below it nothing was left of 131071 keys.)
+//
 // An e4m3 cache: codes are exact in either 16-bit type.  q.code is scaled by the key's power of two
 // in float32.  The value's power of two 2^ev joins the weight, exactly: p 2^(ev - top + kHeadroom), top
 // the largest ev so far.  A large scale says nothing about a row's other channels, so the weights of rows
@@ -107,7 +112,8 @@ __device__ __forceinline__ void attend_tile(const TileData<E4M3>& d, const u32x4
     s[i] = live ? s[i] : kNegInf;
     top = fmaxf(top, s[i]);
   }
-  st.mx = fmaxf(st.mx, max_rows(top));
+  top = max_rows(top);
+  st.mx = fmaxf(st.mx, top);
   const float ref = st.mx == kNegInf ? st.ref : st.mx * kSoftmaxScale2;
   const float alpha = exp2_hw(st.ref - ref);
   st.l *= alpha;
@@ -143,8 +149,22 @@ __device__ __forceinline__ void attend_tile(const TileData<E4M3>& d, const u32x4
       v[i] = u32x4_t{unpack_codes<true, false>(d.v[i][0], 1.0f), unpack_codes<true, true>(d.v[i][0], 1.0f),
                      unpack_codes<true, false>(d.v[i][1], 1.0f), unpack_codes<true, true>(d.v[i][1], 1.0f)};
     pv_tile<true, 3>(st.acc, v, w);
+  } else if constexpr (BF16) {
+    pv_tile<true, 3>(st.acc, d.v, w);
   } else {
-    pv_tile<BF16, BF16 ? 3 : 2>(st.acc, d.v, w);
+    // the largest of the tile's weights to 2^14..2^15, and the tile's sums back by as much
+    const int by = 15 - __builtin_amdgcn_frexp_expf(exp2_hw(fmaf(top, kSoftmaxScale2, -ref)));
+    f32x4_t sum[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = ldexpf(w[i], by);
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) sum[cb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    pv_tile<false>(sum, d.v, w);
+    const float back = ldexpf(1.0f, -by);
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.acc[cb][i] = fmaf(sum[cb][i], back, st.acc[cb][i]);
   }
 }
 

@@ -92,3 +92,31 @@ def test_e4m3_scales_of_rows_that_are_empty_where_it_matters(kv, large, small, d
     out = decode(codes, scales, q, kv, dt)
     # (numbers below 2^-126 are of no account)
     check(out, q, e4m3_rows(codes[0], scales[0], kv), e4m3_rows(codes[1], scales[1], kv), 2.0 ** -24, 2.0 ** -125, dt, (large, small))
+
+
+def one_key_above(kv, at, nats, hkv, dt):
+    """Caches in which one key lies `nats` above all others, which are alike, and its value is 0."""
+    g = torch.Generator(device=DEV).manual_seed(kv + at)
+    pages = -(-kv // 16)
+    k, v = torch.zeros(hkv, pages, 16, S.D, device=DEV), 0.5 + torch.randn(hkv, pages, 16, S.D, generator=g, device=DEV)
+    k.flatten(1, 2)[:, at] = nats / math.sqrt(S.D)
+    v.flatten(1, 2)[:, at] = 0.0
+    return k.to(DT[dt]), v.to(DT[dt])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("nats", [10.0, 17.0, 20.0, 25.0])
+@pytest.mark.parametrize("kv,at", [(1000, 999), (131072, 7)])
+def test_decode_keys_far_below_one(kv, at, nats, dt):
+    """Two float16 terms of a weight are off by 2^-22, or by 2^-39 of the largest weight among the 16 tokens of a tile
+    (subnormal terms): that much of the largest |v| of the channel, for each token."""
+    k, v = one_key_above(kv, at, nats, 2, dt)
+    q = torch.ones(1, 8, S.D, device=DEV, dtype=DT[dt])
+    out = decode((k, v), (None, None), q, kv, dt)
+    k64, v64 = (x.flatten(1, 2)[:, :kv].double() for x in (k, v))
+    werr, floor = 2.0 ** -24, 0.0
+    if dt == "f16":
+        tops = 1.0 + kv / 16 * math.exp(-nats * 0.999)  # (sum over tiles of their largest weights; l > 1)
+        werr, floor = 2.0 ** -22, (2.0 ** -39 * 16 * tops * v64.abs().amax(1)).repeat_interleave(4, 0)
+    check(out, q, k64, v64, werr, floor, dt, nats)
