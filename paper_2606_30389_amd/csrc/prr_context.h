@@ -105,6 +105,13 @@ constexpr float kSoftmaxScale2 = 0.08838834764831845f * kLog2e;
 // 2^x to one unit in the last place; results below the smallest normal number are 0
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Storage of an infinity or a NaN.
+template <bool BF16>
+__device__ __forceinline__ bool non_finite(uint32_t bits16) {
+  constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u;
+  return (bits16 & kExp) == kExp;
+}
+
 // Two floats rounded to nearest even to the 16-bit type, packed.
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float x, float y) {

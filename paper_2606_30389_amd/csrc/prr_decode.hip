@@ -229,24 +229,27 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
   // tile w of the part's runs of NW tiles, every parts-th run
   const int step = parts * NW, first = part * NW + w;
   const int mine = (tiles - first + step - 1) / step;
+  // the first cache row and the tokens of the wave's tile i; no tokens: there is no such tile
+  const auto find = [&](int i, int64_t& row, int& valid) {
+    row = 0;
+    valid = 0;
+    if (i >= mine) return;
+    const int x = first + step * i;
+    const int sub = x & ((1 << sh) - 1);
+    int lp = x >> sh;
+    if (a.pages) lp = a.pages[((size_t)s * a.c.num_kv_heads + h) * a.cap + lp];
+    const int64_t tok = ((int64_t)lp << a.c.page_shift) + sub * kTile;
+    if (lp < 0 || tok >= kv) return;
+    const int phys = phys_page(a.b.page_table, a.b.table_stride, a.c.max_pages, s, lp);
+    if (phys < 0) return;
+    valid = (int)min(kv - tok, (int64_t)kTile);
+    row = head_row + ((int64_t)phys << a.c.page_shift) + sub * kTile;
+  };
   for (int i0 = 0; i0 < mine; i0 += kWave) {
     // where the wave's next 64 tiles lie: lane i looks tile i0 + i up
-    int64_t my_row = 0;
-    int my_valid = 0;
-    if (i0 + lane < mine) {
-      const int x = first + step * (i0 + lane);
-      const int sub = x & ((1 << sh) - 1);
-      int lp = x >> sh;
-      if (a.pages) lp = a.pages[((size_t)s * a.c.num_kv_heads + h) * a.cap + lp];
-      const int64_t tok = ((int64_t)lp << a.c.page_shift) + sub * kTile;
-      if (lp >= 0 && tok < kv) {
-        const int phys = phys_page(a.b.page_table, a.b.table_stride, a.c.max_pages, s, lp);
-        if (phys >= 0) {
-          my_valid = (int)min(kv - tok, (int64_t)kTile);
-          my_row = head_row + ((int64_t)phys << a.c.page_shift) + sub * kTile;
-        }
-      }
-    }
+    int64_t my_row;
+    int my_valid;
+    find(i0 + lane, my_row, my_valid);
     // the valid tiles, in order, the next one's loads ahead of a tile's products
     uint64_t todo = __ballot(my_valid > 0);
     if (!todo) continue;
@@ -276,6 +279,42 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
         attend_tile<BF16, E4M3>(d[x], qf, valid[x], st);
         next(x);
       }
+    }
+  }
+
+  // An infinite value meets weight terms of 0 and of the other sign and comes out as NaN.  Where there is a NaN the
+  // channel is the sum of its values that are not finite, whatever their weights.
+  if constexpr (!E4M3) {
+    bool odd = false;
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) odd |= st.acc[cb][i] != st.acc[cb][i];
+    if (__any(odd)) {
+      f32x4_t sum[8];
+#pragma unroll
+      for (int cb = 0; cb < 8; ++cb) sum[cb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int x = 0; x < mine; ++x) {
+        int64_t row;
+        int valid;
+        find(x, row, valid);
+        for (int r = 0; r < valid; ++r) {
+          const uint16_t* v = static_cast<const uint16_t*>(a.c.v) + (row + r) * kHeadDim + 32 * j;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const u32x4_t y = *reinterpret_cast<const u32x4_t*>(v + 8 * i);
+#pragma unroll
+            for (int cb = 0; cb < 8; ++cb) {
+              const uint32_t bits = (y[cb >> 1] >> (16 * (cb & 1))) & 0xffffu;
+              if (non_finite<BF16>(bits)) sum[cb][i] += h2f<BF16>(bits);
+            }
+          }
+        }
+      }
+#pragma unroll
+      for (int cb = 0; cb < 8; ++cb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st.acc[cb][i] = sum[cb][i] == 0.0f ? st.acc[cb][i] : sum[cb][i];
     }
   }
 

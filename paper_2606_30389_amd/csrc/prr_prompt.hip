@@ -45,12 +45,6 @@ constexpr float kSlack = 8.0f;
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
 template <bool BF16>
-__device__ __forceinline__ bool non_finite(uint32_t bits16) {
-  constexpr uint32_t kExp = BF16 ? 0x7f80u : 0x7c00u;
-  return (bits16 & kExp) == kExp;
-}
-
-template <bool BF16>
 __device__ __forceinline__ f32x16_t mfma32(const u32x4_t& a, const u32x4_t& b, f32x16_t c) {
   if constexpr (BF16) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,

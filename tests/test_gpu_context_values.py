@@ -120,3 +120,31 @@ def test_decode_keys_far_below_one(kv, at, nats, dt):
         tops = 1.0 + kv / 16 * math.exp(-nats * 0.999)  # (sum over tiles of their largest weights; l > 1)
         werr, floor = 2.0 ** -22, (2.0 ** -39 * 16 * tops * v64.abs().amax(1)).repeat_interleave(4, 0)
     check(out, q, k64, v64, werr, floor, dt, nats)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dt", ["bf16", "f16"])
+@pytest.mark.parametrize("kv,at", [(1, 0), (40, 39), (700, 3), (9000, 8123)])
+def test_decode_infinite_values(kv, at, dt):
+    """A value of infinity makes its channel that infinity, two of both signs or a NaN make it NaN; the other channels do
+    not change."""
+    g = torch.Generator(device=DEV).manual_seed(kv)
+    pages = -(-kv // 16)
+    k, v = (torch.randn(2, pages, 16, S.D, generator=g, device=DEV).to(DT[dt]) for _ in range(2))
+    q = torch.randn(1, 8, S.D, generator=g, device=DEV).to(DT[dt])
+    clean = decode((k, v), (None, None), q, kv, dt)
+    dirty = v.clone()
+    rows = dirty.flatten(1, 2)
+    rows[0, at, 5], rows[0, at, 127], rows[0, at, 64] = math.inf, -math.inf, math.nan
+    rows[1, at, 0] = math.inf
+    if kv > 1:
+        rows[0, at - 1, 5], rows[1, at - 1, 0] = math.inf, -math.inf
+    out = decode((k, dirty), (None, None), q, kv, dt)
+    for o in (x[0].float() for x in out[:2]):
+        assert torch.all(o[:4, 5] == math.inf) and torch.all(o[:4, 127] == -math.inf) and torch.all(o[:4, 64].isnan())
+        assert torch.all(o[4:, 0].isnan() if kv > 1 else o[4:, 0] == math.inf)
+    same = torch.ones(8, S.D, dtype=torch.bool, device=DEV)
+    same[:4, [5, 64, 127]] = False
+    same[4:, 0] = False
+    assert all(torch.equal(x[0][same], y[0][same]) for x, y in zip(out[:2], clean[:2]))
+    assert torch.equal(out[2], clean[2]) and torch.equal(out[3], clean[3])
