@@ -368,8 +368,8 @@ prr_status prr_cache_read(const prr_dims* dims, const void* k_codes, const void*
  *   q            device [total_q][Hq][128] dtype
  *   out_o        device [total_q][Hq][128] dtype out
  *   out_m, out_l device [total_q][Hq] float32 out (both or neither NULL)
- * Weights are rounded to the 16-bit type for the product with the values, everything else is
- * float32.  A token that sees no key gets the empty state.  Keys and values that a token does not
+ * Weights are rounded to the 16-bit type for the product with the values (float16: to 2^-36 of the row's largest
+ * where they are subnormal), everything else is float32.  A token that sees no key gets the empty state.  Keys and values that a token does not
  * see do not change its result, infinities and NaN among them.  A page-table entry out of range
  * makes the results of its sequence unspecified.  Workspace: prr_prompt_workspace_size bytes,
  * 256-byte aligned, contents of no account before and after (NULL if that is 0). */

@@ -18,6 +18,9 @@ namespace {
 // V^T's tokens are read in that order, 4 tokens of one channel at a time, by transposing LDS loads.
 // So no weight moves between lanes, and the rescale of a row is local to a lane.
 //
+// The weights are rounded to the 16-bit type, once, as the output is: the largest error of 509 tokens over 65536 is
+// 1.4 times that of float32 weights.  A second term would make 48 products of a tile's 32.
+//
 // K and V tiles lie in LDS row by row, the rows padded by 16 (K) and 64 bytes (V), so that a read of 16
 // bytes of eight rows, or of 32 bytes of four, touches every bank once at an immediate offset
 // (permuted chunks instead: 28% of the LDS cycles were conflicts).  Two buffers each; global loads run
@@ -38,9 +41,14 @@ namespace {
 constexpr int kTokens = 64;
 constexpr int kKPitch = kHeadDim + 8, kVPitch = kHeadDim + 32;  // elements
 constexpr float kNoRef = -3e38f;
-// a row's reference exponent is moved only when its maximum outgrows it by this much (powers of two):
-// weights stay below 2^8, in range of either type, and the accumulators are rarely rescaled
-constexpr float kSlack = 8.0f;
+// A row's weights are relative to a reference exponent that puts its maximum at 2^kTop and is moved only when
+// the maximum outgrows that by 2^kSlack, so that the accumulators are rarely rescaled.  float16 weights lie at
+// the top of their range (below 2^15): their step of 2^-24 is 2^-35 of the row's maximum or less (with the
+// maximum at 1, keys 17 nats below it were counted in the sum but not in the output).
+template <bool BF16>
+constexpr float kTop = BF16 ? 0.0f : 11.0f;
+template <bool BF16>
+constexpr float kSlack = BF16 ? 8.0f : 4.0f;
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
@@ -255,9 +263,9 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
       for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
     mx = fmaxf(mx, max_halves(top));
     const float scaled = mx * kSoftmaxScale2;
-    const bool grown = scaled > ref + kSlack;
+    const bool grown = scaled > ref + (kTop<BF16> + kSlack<BF16>);
     if (__any(grown)) {
-      const float next = grown ? scaled : ref;
+      const float next = grown ? scaled - kTop<BF16> : ref;
       const float alpha = exp2_hw(ref - next);
       ref = next;
       l *= alpha;

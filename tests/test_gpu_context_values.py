@@ -123,6 +123,30 @@ def test_decode_keys_far_below_one(kv, at, nats, dt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("nats", [10.0, 15.0, 17.0, 20.0])
+@pytest.mark.parametrize("kv,new,at", [(1000, 40, 7), (20000, 300, 19000), (1500, 1500, 3)])
+def test_prompt_keys_far_below_one(kv, new, at, nats):
+    """float16 weights of a prompt are off by 2^-11, or by 2^-36 of the row's largest (subnormal)."""
+    import paper_2606_30389_amd as P
+    from paper_2606_30389_amd import runtime as R
+    k, v = one_key_above(kv, at, nats, 2, "f16")
+    pc = R.PathConfig(num_q_heads=4, num_kv_heads=2, page_size=16, num_tokens=kv, k_select=1, dtype="f16")
+    cache = R.PagedCache(pc, DEV, k=k, v=v)
+    q = torch.ones(new, 4, S.D, device=DEV, dtype=torch.float16)
+    got = cache.prompt(R.Batch(DEV, [new], [kv]), q)
+    torch.cuda.synchronize()
+    assert P.PRR_KV_16 == cache.kind
+    pos = torch.arange(kv - new, kv, device=DEV)
+    eps = S.half_step(torch.float16)
+    for h in range(4):
+        k64, v64 = (x.flatten(1, 2)[h // 2, :kv].double() for x in (k, v))
+        seen = torch.arange(kv, device=DEV) <= pos[:, None]
+        o, m, l, a, mag = S.attend64(q[:, h].double(), k64, v64, seen)
+        floor = 2.0 ** -36 * kv * v64.abs().amax(0) / l[:, None] + 2.0 ** -25
+        S.check_state(got[0][:, h].double(), got[1][:, h].double(), got[2][:, h].double(), o, m, l, a, mag, eps, eps, kv, floor, (h, nats))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dt", ["bf16", "f16"])
 @pytest.mark.parametrize("kv,at", [(1, 0), (40, 39), (700, 3), (9000, 8123)])
 def test_decode_infinite_values(kv, at, dt):
