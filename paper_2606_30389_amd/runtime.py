@@ -318,7 +318,8 @@ class LayerState:
     def cache(self) -> PagedCache:
         """This layer's keys and values as a PagedCache (the same memory)."""
         if getattr(self, "_cache", None) is None:
-            self._cache = PagedCache(self.cfg, self.k.device, k=self.k, v=self.v)
+            # (as many pages as the layer has, whatever its tokens are by now)
+            self._cache = PagedCache(dataclasses.replace(self.cfg, max_pages=self.dims.max_pages), self.k.device, k=self.k, v=self.v)
         return self._cache
 
     def batch(self, new_tokens) -> Batch:

@@ -1,0 +1,49 @@
+"""PagedCache, Batch and LayerState on streams of their own, in graphs, and as a sequence grows."""
+import math
+
+import pytest
+import torch
+
+from tests import context_support as S
+
+DEV = "cuda:0"
+
+
+def busy(stream, ms=20):
+    """Work on `stream` that takes some time."""
+    with torch.cuda.stream(stream):
+        x = torch.ones(4096, 4096, device=DEV)
+        for _ in range(ms):
+            x = x @ x * 1e-4
+    return x
+
+
+def layer(tokens, hq=8, hkv=2, page=16, **kw):
+    from paper_2606_30389_amd import runtime as R
+    return R.LayerState(R.PathConfig(num_q_heads=hq, num_kv_heads=hkv, page_size=page, num_tokens=tokens, k_select=4, **kw), DEV)
+
+
+def rand(*shape, seed=0, dtype=torch.bfloat16):
+    return torch.randn(*shape, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV).to(dtype)
+
+
+@pytest.mark.gpu
+def test_layer_of_fewer_tokens_than_it_was_made_for():
+    """A layer made for 4096 tokens holds 1000, then 1001."""
+    from paper_2606_30389_amd import runtime as R
+    st, ref = layer(4096), layer(1001)
+    qkv = rand(1001, 12, S.D, seed=2)
+    q, k, v = qkv[:, :8], qkv[:, 8:10], qkv[:, 10:]
+    stack = R.DecodeStack([st], [q[-1].contiguous()], DEV)
+    stack.set_tokens(1000)
+    out = st.prefill(q[:1000], k[:1000], v[:1000])
+    stack.set_tokens(1001)
+    st.append(q[1000:], k[1000:], v[1000:])
+    ref.prefill(q, k, v)
+    want = layer(1000).prefill(q[:1000], k[:1000], v[:1000])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(out, want))
+    pages = ref.k.shape[1]
+    assert torch.equal(st.k[:, :pages], ref.k) and torch.equal(st.v[:, :pages], ref.v)
+    assert torch.equal(st.meta[:, :pages], ref.meta)
+    assert torch.all(st.k[:, pages:] == 0)
