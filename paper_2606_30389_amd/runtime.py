@@ -322,16 +322,18 @@ class LayerState:
             self._cache = PagedCache(dataclasses.replace(self.cfg, max_pages=self.dims.max_pages), self.k.device, k=self.k, v=self.v)
         return self._cache
 
-    def batch(self, new_tokens) -> Batch:
-        """The layer's sequence with `new_tokens` new ones at the end of its cfg.num_tokens."""
+    def batch(self, new_tokens, stream=None) -> Batch:
+        """The layer's sequence with `new_tokens` new ones at the end of its cfg.num_tokens, for calls on `stream`: its
+        lengths are uploaded there, and their memory goes back there."""
         table = None if self.page_table is None else self.page_table.view(1, -1)
-        return Batch(self.k.device, [new_tokens], [self.cfg.num_tokens], table)
+        with _stream_context(stream, self.k.device):
+            return Batch(self.k.device, [new_tokens], [self.cfg.num_tokens], table)
 
     def prefill(self, q, k, v, rope: Optional[Rope] = None, batch: Optional[Batch] = None, stream=None):
         """The last len(q) of the cfg.num_tokens tokens: into the cache, their causal attention, and the metadata
         of the pages that they touch.  q [n][Hq][128], k, v [n][Hkv][128]; returns (o, m, l)."""
         cfg = self.cfg
-        batch = self.batch(q.shape[0]) if batch is None else batch
+        batch = self.batch(q.shape[0], stream) if batch is None else batch
         q = self.cache().append(batch, q, k, v, rope, stream=stream)
         out = self.cache().prompt(batch, q, stream=stream)
         self.build_meta(stream, page_begin=(cfg.num_tokens - q.shape[0]) // cfg.page_size)
@@ -341,7 +343,7 @@ class LayerState:
         """One new token, the last of the cfg.num_tokens: into the cache, and its page's metadata; returns the
         rotated query, ready for select() or a decode step."""
         cfg = self.cfg
-        q = self.cache().append(self.batch(1) if batch is None else batch, q, k, v, rope, q_out=q_out, stream=stream)
+        q = self.cache().append(self.batch(1, stream) if batch is None else batch, q, k, v, rope, q_out=q_out, stream=stream)
         self.build_meta(stream, page_begin=(cfg.num_tokens - 1) // cfg.page_size)
         return q
 

@@ -47,3 +47,35 @@ def test_layer_of_fewer_tokens_than_it_was_made_for():
     assert torch.equal(st.k[:, :pages], ref.k) and torch.equal(st.v[:, :pages], ref.v)
     assert torch.equal(st.meta[:, :pages], ref.meta)
     assert torch.all(st.k[:, pages:] == 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("by_address", [False, True])
+def test_layer_calls_without_a_batch_on_another_stream(by_address):
+    """prefill and append make their batch for the stream of the call: what the current stream allocates meanwhile does
+    not get its memory."""
+    n0, n = 100, 130
+    st, ref = layer(n), layer(n)
+    qkv = rand(n, 12, S.D, seed=1)
+    q, k, v = qkv[:, :8], qkv[:, 8:10], qkv[:, 10:]
+    stream = torch.cuda.Stream()
+    given = stream.cuda_stream if by_address else stream
+    torch.cuda.synchronize()
+    held = busy(stream)
+    st.cfg.num_tokens = ref.cfg.num_tokens = n0
+    out = st.prefill(q[:n0], k[:n0], v[:n0], stream=given)
+    scribble = [torch.full((2,), 7 + i, dtype=torch.int32, device=DEV) for i in range(64)]
+    for t in range(n0, n):
+        st.cfg.num_tokens = t + 1
+        st.append(q[t:t + 1], k[t:t + 1], v[t:t + 1], stream=given)
+        scribble.append(torch.full((1,), 3, dtype=torch.int32, device=DEV))
+        scribble.append(torch.full((2,), 3, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    want = ref.prefill(q[:n0], k[:n0], v[:n0])
+    ref.cfg.num_tokens = n
+    ref.build_meta()
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(out, want))
+    assert torch.equal(st.k.flatten(1, 2)[:, :n], k.transpose(0, 1)) and torch.equal(st.v.flatten(1, 2)[:, :n], v.transpose(0, 1))
+    assert torch.all(st.k.flatten(1, 2)[:, n:] == 0)
+    del held
