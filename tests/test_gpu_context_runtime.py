@@ -79,3 +79,57 @@ def test_layer_calls_without_a_batch_on_another_stream(by_address):
     assert torch.equal(st.k.flatten(1, 2)[:, :n], k.transpose(0, 1)) and torch.equal(st.v.flatten(1, 2)[:, :n], v.transpose(0, 1))
     assert torch.all(st.k.flatten(1, 2)[:, n:] == 0)
     del held
+
+
+@pytest.mark.gpu
+def test_two_graphs_of_one_cache_replayed_at_once():
+    """Two prompts and a token's attention, each split into parts, captured on the one stream that captures use and replayed on
+    streams of their own at the same time, eager calls in between."""
+    from paper_2606_30389_amd import _lib as L
+    from paper_2606_30389_amd import runtime as R
+    tokens = 40000
+    pc = R.PathConfig(num_q_heads=16, num_kv_heads=1, page_size=16, num_tokens=tokens, k_select=1)
+    cache = R.PagedCache(pc, DEV)
+    cache.k.copy_(rand(*cache.k.shape, seed=3))
+    cache.v.copy_(rand(*cache.v.shape, seed=4))
+    batches = [R.Batch(DEV, [16], [tokens]), R.Batch(DEV, [16], [tokens - 5]), R.Batch(DEV, [1], [tokens])]
+    assert L.prr_prompt_workspace_size(cache.dims, batches[0].native) and L.prr_decode_workspace_size(cache.dims, batches[2].native, 0)
+    qs = [rand(16, 16, S.D, seed=5), rand(16, 16, S.D, seed=6), rand(1, 16, S.D, seed=7)]
+    call = [cache.prompt, cache.prompt, cache.attend]
+    want = [f(b, q) for f, b, q in zip(call, batches, qs)]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for f, b, q in zip(call, batches, qs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(f(b, q))
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for _ in range(20):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        got = [f(b, q) for f, b, q in zip(call, batches, qs)]
+        torch.cuda.synchronize()
+        for g, o, w in zip(got, outs, want):
+            assert all(torch.equal(x, y) for x, y in zip(g, w)) and all(torch.equal(x, y) for x, y in zip(o, w))
+            for x in o:
+                x.fill_(2.0)
+        torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+def test_workspaces_are_not_kept():
+    """Calls that need ever larger workspaces, on two streams, leave nothing allocated behind."""
+    from paper_2606_30389_amd import runtime as R
+    pc = R.PathConfig(num_q_heads=16, num_kv_heads=1, page_size=16, num_tokens=65536, k_select=1)
+    cache, other = R.PagedCache(pc, DEV), torch.cuda.Stream()
+    q = rand(64, 16, S.D, seed=8)
+    batches = [R.Batch(DEV, [64], [n]) for n in (4096, 16384, 65536)]
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    for b in batches:
+        cache.prompt(b, q)
+        cache.prompt(b, q, stream=other)
+        cache.prompt(b, q, stream=other.cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() == before
