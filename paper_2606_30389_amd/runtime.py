@@ -94,12 +94,16 @@ class Rope:
 class Batch:
     """The sequences of a call: their new tokens, their tokens in the cache (the new ones included) and
     their rows of the page table.  The lengths live on the device (cu_q, kv_len), where a captured graph
-    reads them; max_q and max_kv bound them for as long as the batch is used."""
+    reads them; max_q, max_kv and total_q (rows of the packed tensors) bound them for as long as the batch is
+    used: the device cuts what is beyond."""
 
     def __init__(self, device, new: Sequence[int], kv: Sequence[int], page_table=None, max_q=None, max_kv=None, total_q=None):
         if len(new) != len(kv) or not len(new) or min(new) < 0 or min(kv) < 0:
             raise ValueError("new and kv: lengths of the same sequences, at least one, none negative")
         cu = np.concatenate([[0], np.cumsum(np.asarray(new, dtype=np.int64))]).astype(np.int32)
+        for name, bound, least in (("max_q", max_q, max(new)), ("max_kv", max_kv, max(kv)), ("total_q", total_q, int(cu[-1]))):
+            if bound is not None and bound < least:
+                raise ValueError(f"{name} {bound}: the lengths need {least}")
         self._longest, self._max_kv = max(kv), max(kv) if max_kv is None else max_kv
         self.kv_len = torch.tensor(list(kv), dtype=torch.int32, device=device)
         if page_table is not None:
