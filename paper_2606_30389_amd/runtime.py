@@ -174,7 +174,9 @@ class PagedCache:
     A call's workspace, and outputs that are not given, are allocated on the call's stream; the workspace goes back
     there when the call returns.  So calls on other streams never share one, and a captured graph has its own, in its pool."""
 
-    def __init__(self, cfg: PathConfig, device, kind="16", k=None, v=None):
+    def __init__(self, cfg: PathConfig, device, kind="16", k=None, v=None, k_scale=None, v_scale=None):
+        """k, v: given caches (e4m3 codes with k_scale, v_scale, the exponent bytes of their rows' powers of two), or None
+        for empty ones."""
         self.cfg, self.dims = cfg, cfg.dims()
         self.kind = {"16": L.PRR_KV_16, "e4m3": L.PRR_KV_E4M3}[kind]
         shape = (cfg.num_kv_heads, self.dims.max_pages, cfg.page_size, 128)
@@ -186,10 +188,18 @@ class PagedCache:
             _check(x, name, shape, dtype, self.k.device)
         if self.k.device.type != torch.device(device).type:
             raise ValueError(f"k: on {self.k.device}, expected on {device}")
-        self.k_scale = self.v_scale = None
-        if kind == "e4m3":  # (exponent bytes of the rows' powers of two: 127 is 1)
-            self.k_scale = torch.full(shape[:3], 127, dtype=torch.uint8, device=self.k.device)
-            self.v_scale = torch.full(shape[:3], 127, dtype=torch.uint8, device=self.k.device)
+        for x, scale, name in ((k, k_scale, "k_scale"), (v, v_scale, "v_scale")):
+            if kind == "e4m3" and (x is None) != (scale is None):
+                raise ValueError(f"{name}: codes come with their scales, or neither is given")
+            if scale is not None:
+                if kind != "e4m3":
+                    raise ValueError(f"{name}: a 16-bit cache has no scales")
+                _check(scale, name, shape[:3], torch.uint8, self.k.device)
+        self.k_scale, self.v_scale = k_scale, v_scale
+        if kind == "e4m3":  # (127 is 1)
+            empty = lambda: torch.full(shape[:3], 127, dtype=torch.uint8, device=self.k.device)  # noqa: E731
+            self.k_scale = empty() if k_scale is None else k_scale
+            self.v_scale = empty() if v_scale is None else v_scale
 
     def _check_batch(self, batch, q):
         """The device of the batch's lengths; the queries of a call that attends."""

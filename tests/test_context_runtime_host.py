@@ -18,3 +18,22 @@ def test_bounds_of_a_batch_hold_its_lengths(over):
         R.Batch("cpu", [5, 3], [5000, 3000], table, **over)
     b = R.Batch("cpu", [5, 3], [5000, 3000], table, max_kv=5000, max_q=5, total_q=8)
     assert (b.native.max_kv, b.native.max_q, b.native.total_q) == (5000, 5, 8)
+
+
+def test_given_codes_come_with_their_scales():
+    pc = R.PathConfig(num_q_heads=4, num_kv_heads=2, page_size=16, num_tokens=64, k_select=1)
+    code = torch.zeros(2, 4, 16, 128, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    scale = torch.full((2, 4, 16), 120, dtype=torch.uint8)
+    for over in (dict(k=code), dict(k=code, v=code), dict(k=code, v=code, k_scale=scale), dict(k_scale=scale), dict(v_scale=scale),
+                 dict(k=code, v=code, k_scale=scale, v_scale=scale[:, :3]), dict(k=code, v=code, k_scale=scale.int(), v_scale=scale),
+                 dict(k=code, v=code, k_scale=scale.to("meta"), v_scale=scale), dict(k=code, v=code, k_scale=scale[..., ::2], v_scale=scale)):
+        with pytest.raises(ValueError):
+            R.PagedCache(pc, "cpu", kind="e4m3", **over)
+    with pytest.raises(ValueError):
+        R.PagedCache(pc, "cpu", k_scale=scale)
+    c = R.PagedCache(pc, "cpu", kind="e4m3", k=code, v=code, k_scale=scale, v_scale=scale.clone())
+    assert c.k_scale is scale and c.k is code and torch.all(c.v_scale == 120)
+    c = R.PagedCache(pc, "cpu", kind="e4m3", k=code, k_scale=scale)
+    assert c.k_scale is scale and torch.all(c.v_scale == 127) and not c.v.view(torch.uint8).any()
+    c = R.PagedCache(pc, "cpu", kind="e4m3")
+    assert torch.all(c.k_scale == 127) and torch.all(c.v_scale == 127)

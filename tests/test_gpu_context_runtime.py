@@ -133,3 +133,19 @@ def test_workspaces_are_not_kept():
         cache.prompt(b, q, stream=other.cuda_stream)
     torch.cuda.synchronize()
     assert torch.cuda.memory_allocated() == before
+
+
+@pytest.mark.gpu
+def test_cache_of_given_codes_and_scales():
+    """An e4m3 cache made from another's codes and scales answers as that one."""
+    from paper_2606_30389_amd import runtime as R
+    pc = R.PathConfig(num_q_heads=8, num_kv_heads=2, page_size=16, num_tokens=320, k_select=1)
+    one = R.PagedCache(pc, DEV, kind="e4m3")
+    one.append(R.Batch(DEV, [300], [300]), None, 5 * rand(300, 2, S.D, seed=9), 0.1 * rand(300, 2, S.D, seed=10))
+    two = R.PagedCache(pc, DEV, kind="e4m3", k=one.k, v=one.v, k_scale=one.k_scale, v_scale=one.v_scale)
+    b, q = R.Batch(DEV, [1], [300]), rand(1, 8, S.D, seed=11)
+    got, want = two.attend(b, q), one.attend(b, q)
+    torch.cuda.synchronize()
+    assert one.k_scale[:, :18].unique().numel() > 1
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert all(torch.equal(x, y) for x, y in zip(two.read(300), one.read(300)))
