@@ -77,17 +77,21 @@ def bits_tensor(bits: np.ndarray, dtype: torch.dtype, device) -> torch.Tensor:
 
 
 class Rope:
-    """Rotary positions of a model: frequencies (prr_rope_freqs, or given) on the device, layout and scale."""
+    """Rotary positions of a model: frequencies (prr_rope_freqs, or given: one per pair) on the device, layout and scale
+    (None: that of the frequencies' rule, 1 for given ones)."""
 
     KINDS = {"plain": L.PRR_ROPE_PLAIN, "linear": L.PRR_ROPE_LINEAR, "ntk": L.PRR_ROPE_NTK,
              "by_parts": L.PRR_ROPE_BY_PARTS, "yarn": L.PRR_ROPE_YARN}
 
     def __init__(self, device, rot_dim=128, base=10000.0, kind="plain", factor=1.0, trained_len=1, lo=1.0, hi=32.0,
-                 interleaved=False, freqs=None, scale=1.0):
+                 interleaved=False, freqs=None, scale=None):
+        rule = 1.0
         if freqs is None:
-            freqs, scale = L.prr_rope_freqs(self.KINDS[kind], rot_dim, base, factor, trained_len, lo, hi)
-        self.freqs = torch.as_tensor(freqs, dtype=torch.float64).to(device)
-        self.rot_dim, self.scale = 2 * self.freqs.numel(), float(scale)
+            freqs, rule = L.prr_rope_freqs(self.KINDS[kind], rot_dim, base, factor, trained_len, lo, hi)
+        self.freqs = torch.as_tensor(freqs, dtype=torch.float64).to(device).contiguous()
+        if self.freqs.dim() != 1 or not len(self.freqs):
+            raise ValueError(f"freqs: shape {tuple(self.freqs.shape)}, expected one number per pair")
+        self.rot_dim, self.scale = 2 * self.freqs.numel(), float(rule if scale is None else scale)
         self.layout = L.PRR_ROPE_INTERLEAVED if interleaved else L.PRR_ROPE_HALF
 
 

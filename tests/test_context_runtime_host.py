@@ -37,3 +37,19 @@ def test_given_codes_come_with_their_scales():
     assert c.k_scale is scale and torch.all(c.v_scale == 127) and not c.v.view(torch.uint8).any()
     c = R.PagedCache(pc, "cpu", kind="e4m3")
     assert torch.all(c.k_scale == 127) and torch.all(c.v_scale == 127)
+
+
+def test_rope_of_given_frequencies():
+    """Frequencies of any strides and types, and a scale that is asked for, arrive as they are."""
+    w = torch.arange(1, 33, dtype=torch.float64) / 64
+    for given in (w, w.numpy(), w.tolist(), w.float(), torch.stack((w, -w), 1)[:, 0], w.flip(0).flip(0)):
+        r = R.Rope("cpu", freqs=given, scale=0.5)
+        assert r.freqs.is_contiguous() and r.freqs.dtype == torch.float64 and torch.equal(r.freqs, w)
+        assert r.rot_dim == 64 and r.scale == 0.5
+    yarn = dict(rot_dim=64, kind="yarn", factor=4.0, trained_len=128)
+    assert R.Rope("cpu", **yarn).scale == pytest.approx(0.1 * math.log(4.0) + 1)
+    assert R.Rope("cpu", **yarn, scale=1.0).scale == 1.0 and R.Rope("cpu", rot_dim=64, scale=0.25).scale == 0.25
+    assert R.Rope("cpu").scale == 1.0 and R.Rope("cpu", freqs=w).scale == 1.0
+    for bad in (w.view(4, 8), w[:0]):
+        with pytest.raises(ValueError):
+            R.Rope("cpu", freqs=bad)
