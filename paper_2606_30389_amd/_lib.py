@@ -318,8 +318,10 @@ _torch = None
 def _on_device(fn, like, stream, *args):
     """fn(*args, stream) with `like`'s device current; stream None = that device's current stream."""
     global _torch
-    if not getattr(like, "is_cuda", False):
+    if like is None or isinstance(like, int):
         return _check(fn(*args, _stream(stream)))
+    if not like.is_cuda:
+        raise ValueError(f"a tensor on {like.device}: these calls take the GPU's memory")
     if _torch is None:
         import torch as _torch
     index = like.get_device()

@@ -53,3 +53,25 @@ def test_rope_of_given_frequencies():
     for bad in (w.view(4, 8), w[:0]):
         with pytest.raises(ValueError):
             R.Rope("cpu", freqs=bad)
+
+
+def test_tensors_of_host_memory_are_not_launched_on():
+    """Everything agrees but lies in host memory: refused by the runtime and by the binding."""
+    pc = R.PathConfig(num_q_heads=4, num_kv_heads=2, page_size=16, num_tokens=64, k_select=1)
+    c, e = R.PagedCache(pc, "cpu"), R.PagedCache(pc, "cpu", kind="e4m3")
+    q, k = torch.zeros(1, 4, 128, dtype=torch.bfloat16), torch.zeros(1, 2, 128, dtype=torch.bfloat16)
+    ml, o32, pages = torch.zeros(1, 4), torch.zeros(1, 4, 128), torch.zeros(2, 4, 16, 128, dtype=torch.bfloat16)
+    b = R.Batch("cpu", [1], [9])
+    for call in (lambda: c.append(b, q, k, k), lambda: c.append(b, q, k, k, q_out=q), lambda: e.append(b, None, k, k), lambda: c.prompt(b, q),
+                 lambda: c.prompt(b, q, out=(q, ml, ml)), lambda: c.attend(b, q), lambda: c.attend(b, q, out=(o32, q, ml, ml)),
+                 lambda: e.read(9), lambda: e.read(9, page_begin=0, page_end=4, out=(pages, pages))):
+        with pytest.raises(ValueError):
+            call()
+    none = dict(stream=0)
+    for call in (lambda: L.prr_rope_append(c.dims, b.native, q, k, k, None, None, 0, 0, 1.0, q, 0, c.k, c.v, **none),
+                 lambda: L.prr_rope_append(c.dims, b.native, None, k, k, None, None, 0, 0, 1.0, None, 0, c.k, c.v, **none),
+                 lambda: L.prr_prompt_attn(c.dims, b.native, q, c.k, c.v, q, ml, ml, None, 0, **none),
+                 lambda: L.prr_decode_attn(c.dims, b.native, q, 0, c.k, c.v, None, None, None, None, 0, o32, q, ml, ml, None, 0, **none),
+                 lambda: L.prr_cache_read(e.dims, e.k, e.v, e.k_scale, e.v_scale, None, 9, 0, 1, pages, pages, **none)):
+        with pytest.raises(ValueError):
+            call()
