@@ -132,10 +132,14 @@ prr_status plan(const prr_dims* d, const prr_batch* b, prr::PromptLaunch& a) {
   a.max_pages = d->max_pages;
   a.page_shift = log2_of(d->page_size);
   a.bf16 = d->dtype == PRR_BF16;
-  // (128 GiB of queries; keeps the grid's threads below 2^32)
+  // (128 GiB of queries)
   if ((int64_t)a.b.total_q * d->num_q_heads > ((int64_t)1 << 29))
     return api_fail(PRR_ERR_UNSUPPORTED, "%d rows x %d heads: more than 2^29", a.b.total_q, d->num_q_heads);
   prr::plan_prompt(a);
+  const int64_t groups = (int64_t)a.tiles * a.num_kv_heads;
+  if (groups * a.waves * 64 >= (int64_t)1 << 32)
+    return api_fail(PRR_ERR_UNSUPPORTED, "%d sequences, %d rows and %d KV heads: %lld workgroups of %d waves", a.b.n_seqs,
+                    a.b.total_q, a.num_kv_heads, (long long)groups, a.waves);
   return PRR_OK;
 }
 

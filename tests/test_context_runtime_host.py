@@ -75,3 +75,14 @@ def test_tensors_of_host_memory_are_not_launched_on():
                  lambda: L.prr_cache_read(e.dims, e.k, e.v, e.k_scale, e.v_scale, None, 9, 0, 1, pages, pages, **none)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("heads,kv,ok", [(4096, 4096, False), (4096, 512, False), (1024, 4096, True), (4096, 0, False)])
+def test_prompt_grids_have_a_limit(heads, kv, ok):
+    """A launch has less than 2^32 threads: 4096 sequences of one token with 4096 KV heads are refused before it."""
+    d = L.make_dims(heads, heads, 16, 256, L.PRR_BF16)
+    fake = 0x10000
+    b = L.make_batch(4096, 4096, 1, kv, None, fake, fake, 256)
+    with pytest.raises(L.PrrError) as e:  # (q missing, where the sizes are accepted)
+        L.prr_prompt_attn(d, b, None, fake, fake, fake, None, None, None, 0, stream=0)
+    assert e.value.status == (L.PRR_ERR_INVALID_ARG if ok else L.PRR_ERR_UNSUPPORTED)
