@@ -363,21 +363,29 @@ class LayerState:
         with _stream_context(stream, self.k.device):
             return Batch(self.k.device, [new_tokens], [self.cfg.num_tokens], table)
 
+    def _one(self, batch, new_tokens, stream):
+        if batch is not None and batch.native.n_seqs != 1:
+            raise ValueError(f"a batch of {batch.native.n_seqs} sequences: a layer holds one")
+        return self.batch(new_tokens, stream) if batch is None else batch
+
     def prefill(self, q, k, v, rope: Optional[Rope] = None, batch: Optional[Batch] = None, stream=None):
         """The last len(q) of the cfg.num_tokens tokens: into the cache, their causal attention, and the metadata
-        of the pages that they touch.  q [n][Hq][128], k, v [n][Hkv][128]; returns (o, m, l)."""
+        of the pages that they touch.  q [n][Hq][128], k, v [n][Hkv][128]; returns (o, m, l).  A given batch holds
+        this one sequence, of cfg.num_tokens tokens; its rows may be more than its new tokens."""
         cfg = self.cfg
-        batch = self.batch(q.shape[0], stream) if batch is None else batch
+        batch = self._one(batch, q.shape[0], stream)
         q = self.cache().append(batch, q, k, v, rope, stream=stream)
         out = self.cache().prompt(batch, q, stream=stream)
-        self.build_meta(stream, page_begin=(cfg.num_tokens - q.shape[0]) // cfg.page_size)
+        # (rows behind the tokens, and tokens without a place, count for none)
+        self.build_meta(stream, page_begin=max(0, cfg.num_tokens - q.shape[0]) // cfg.page_size)
         return out
 
     def append(self, q, k, v, rope: Optional[Rope] = None, batch: Optional[Batch] = None, q_out=None, stream=None):
         """One new token, the last of the cfg.num_tokens: into the cache, and its page's metadata; returns the
-        rotated query, ready for select() or a decode step."""
+        rotated query, ready for select() or a decode step.  The metadata's page is that of this moment: a captured graph
+        keeps it."""
         cfg = self.cfg
-        q = self.cache().append(self.batch(1, stream) if batch is None else batch, q, k, v, rope, q_out=q_out, stream=stream)
+        q = self.cache().append(self._one(batch, 1, stream), q, k, v, rope, q_out=q_out, stream=stream)
         self.build_meta(stream, page_begin=(cfg.num_tokens - 1) // cfg.page_size)
         return q
 

@@ -149,3 +149,41 @@ def test_cache_of_given_codes_and_scales():
     assert one.k_scale[:, :18].unique().numel() > 1
     assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert all(torch.equal(x, y) for x, y in zip(two.read(300), one.read(300)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,new,rows", [(40, 40, 64), (200, 3, 512), (33, 0, 5)])
+def test_prefill_with_rows_behind_the_sequence(n, new, rows):
+    """A given batch with more rows than tokens: the tokens are served, the rows behind them are left, and the metadata is that of
+    the whole context."""
+    from paper_2606_30389_amd import runtime as R
+    st, ref = layer(n), layer(n)
+    for x in (st, ref):
+        x.k.copy_(rand(*x.k.shape, seed=12))
+        x.v.copy_(rand(*x.v.shape, seed=13))
+        x.build_meta()
+    q, k, v = rand(rows, 8, S.D, seed=14), rand(rows, 2, S.D, seed=15), rand(rows, 2, S.D, seed=16)
+    out = st.prefill(q, k, v, batch=R.Batch(DEV, [new], [n], total_q=rows))
+    torch.cuda.synchronize()
+    for x in out:
+        assert torch.all(x[new:] == 0)
+    if new:
+        want = ref.prefill(q[:new].contiguous(), k[:new], v[:new])
+        torch.cuda.synchronize()
+        assert all(torch.equal(x[:new], y) for x, y in zip(out, want))
+    assert torch.equal(st.k, ref.k) and torch.equal(st.meta, ref.meta)
+
+
+@pytest.mark.gpu
+def test_layers_serve_one_sequence():
+    from paper_2606_30389_amd import runtime as R
+    st = layer(64)
+    before = st.k.clone()
+    table = torch.arange(8, dtype=torch.int32, device=DEV).view(2, 4) % 4
+    two = R.Batch(DEV, [1, 1], [30, 20], table)
+    q, k = rand(2, 8, S.D), rand(2, 2, S.D)
+    for call in (lambda: st.prefill(q, k, k, batch=two), lambda: st.append(q, k, k, batch=two)):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert torch.equal(st.k, before)
