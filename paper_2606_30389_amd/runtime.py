@@ -64,9 +64,11 @@ class PathConfig:
                            L.PRR_META_MEAN if self.meta_kind == "mean" else L.PRR_META_MINMAX)
 
     def list_cap(self):
+        """Entries of the longest list, for as many tokens as the pages can hold."""
         nf = len(self.forced)
+        pages = self.max_pages or self.num_pages
         def size(k):
-            return min(self.num_pages, max(k, nf) if self.forced_in_budget else k + nf)
+            return min(pages, max(k, nf) if self.forced_in_budget else k + nf)
         return max(1, size(self.k_select), size(self.p_select if self.p_select is not None else self.k_select))
 
 
@@ -533,10 +535,14 @@ class DecodeStack:
             self.io[i].theta = None if st.theta is None else st.theta.ctypes.data
 
     def set_tokens(self, num_tokens):
-        """The sequence now holds num_tokens tokens: for the next steps of every layer."""
+        """The sequence now holds num_tokens tokens (as many as the layers' pages hold): for the next steps of every
+        layer.  Graphs that were captured keep the tokens of their capture."""
+        if not 1 <= num_tokens <= self.dims.max_pages * self.dims.page_size:
+            raise ValueError(f"{num_tokens} tokens: the layers hold 1 to {self.dims.max_pages * self.dims.page_size}")
         for st in self.layers:
             st.cfg.num_tokens = num_tokens
-        self.params.num_tokens, self.params.num_pages = self.cfg.num_tokens, self.cfg.num_pages
+        cfg = self.layers[0].cfg
+        self.params.num_tokens, self.params.num_pages = cfg.num_tokens, cfg.num_pages
 
     def _parity(self):
         parity = self.layers[0].cur

@@ -187,3 +187,44 @@ def test_layers_serve_one_sequence():
             call()
     torch.cuda.synchronize()
     assert torch.equal(st.k, before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("schedule", ["serial", "fused"])
+def test_a_layer_grows_to_its_pages(schedule):
+    """A layer of 20 tokens with room for 512, a budget of 8 pages: appended and stepped until it has 300, the step attends
+    what is selected."""
+    import paper_2606_30389_amd as P
+    from paper_2606_30389_amd import runtime as R
+    n0, n, hq, hkv = 20, 300, 8, 2
+    pc = R.PathConfig(num_q_heads=hq, num_kv_heads=hkv, page_size=16, num_tokens=n0, k_select=8, max_pages=32)
+    st = R.LayerState(pc, DEV)
+    qbuf = torch.empty(1, hq, S.D, dtype=torch.bfloat16, device=DEV)
+    stack = R.DecodeStack([st], [qbuf], DEV)
+    qkv = rand(n, hq + 2 * hkv, S.D, seed=17)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    st.prefill(q[:n0], k[:n0], v[:n0])
+    one = R.Batch(DEV, [1], [n0], max_kv=512)
+    s = torch.cuda.current_stream()
+    for t in range(n0, n):
+        stack.set_tokens(t + 1)
+        one.advance()
+        st.append(q[t:t + 1], k[t:t + 1], v[t:t + 1], batch=one, q_out=qbuf)
+        if schedule == "serial":
+            stack.step(P.PRR_SCHED_FUSED_SERIAL, s)
+        else:
+            stack.step(P.PRR_SCHED_FUSED_PREFILL if t == n0 else P.PRR_SCHED_FUSED_PRR, s)
+            if t == n0:
+                continue
+        if t % 29 and t != n - 1:
+            continue
+        torch.cuda.synchronize()
+        assert st.sel_count.tolist() == [min(8, -(-(t + 1) // 16))] * hkv
+        listed = st.cache().attend(one, qbuf, st.sel[None].contiguous(), st.sel_count[None].contiguous())
+        torch.cuda.synchronize()
+        # the same keys in float32, by two kernels: 2^-15 of the values' size
+        assert (st.out_o32 - listed[0][0]).abs().max() <= 2.0 ** -15 * v.abs().max()
+        assert torch.allclose(st.out_m, listed[2][0], rtol=1e-5, atol=1e-5)
+    with pytest.raises(ValueError):
+        stack.set_tokens(513)
+    assert pc.num_tokens == n
