@@ -360,9 +360,11 @@ class LayerState:
 
     def batch(self, new_tokens, stream=None) -> Batch:
         """The layer's sequence with `new_tokens` new ones at the end of its cfg.num_tokens, for calls on `stream`: its
-        lengths are uploaded there, and their memory goes back there."""
+        lengths are uploaded there, and their memory goes back there (so not in a capture)."""
         table = None if self.page_table is None else self.page_table.view(1, -1)
         with _stream_context(stream, self.k.device):
+            if torch.cuda.is_current_stream_capturing():
+                raise ValueError("a captured call needs a batch made before: its lengths are uploaded")
             return Batch(self.k.device, [new_tokens], [self.cfg.num_tokens], table)
 
     def _one(self, batch, new_tokens, stream):

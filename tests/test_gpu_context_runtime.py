@@ -228,3 +228,30 @@ def test_a_layer_grows_to_its_pages(schedule):
     with pytest.raises(ValueError):
         stack.set_tokens(513)
     assert pc.num_tokens == n
+
+
+@pytest.mark.gpu
+def test_captured_layer_calls_need_a_batch():
+    """Without one they are refused, and the capture goes on; with one, the replays follow the batch's lengths."""
+    from paper_2606_30389_amd import runtime as R
+    st = layer(64)
+    q, k = rand(1, 8, S.D, seed=18), rand(1, 2, S.D, seed=19)
+    one, qbuf = R.Batch(DEV, [1], [60], max_kv=64), torch.empty_like(q)
+    out = [torch.empty(1, 8, S.D, device=DEV), None, torch.empty(1, 8, device=DEV), torch.empty(1, 8, device=DEV)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(ValueError):
+            st.append(q, k, k)
+        one.advance()
+        st.append(q, k, k, batch=one, q_out=qbuf)
+        st.cache().attend(one, qbuf, out=out)
+    for t in range(61, 65):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert int(one.kv_len) == t
+        filled = st.k.flatten(1, 2)[:, 60:].ne(0).any(-1)
+        assert torch.all(filled[:, :t - 60]) and not filled[:, t - 60:].any()
+        want = st.cache().attend(R.Batch(DEV, [1], [t], max_kv=64), qbuf)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip([out[0], *out[2:]], [want[0], *want[2:]]))
