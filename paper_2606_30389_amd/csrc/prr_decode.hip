@@ -7,16 +7,16 @@ namespace {
 
 // The keys of a (sequence, KV head) are cut into tiles of 16 tokens, the tiles into runs of eight, and the
 // runs are dealt out to the parts, one workgroup of eight waves each, so that all workgroups read one
-// moving window of the cache (parts of consecutive tokens: 32 sequences of up to 16K tokens 250 us, dealt
-// out 244; 64 MiB read so by the bare loads 11.7 us, by 2048 workgroups 13.4).  Wave w takes tile w of
+// moving window of the cache (parts of consecutive tokens are 2% slower).  Wave w takes tile w of
 // each run with an online softmax of its own, the next tile's loads issued before a tile is computed (more
-// in flight is no faster: the loads alone take 18.7 us of the 19.3 of 2 x 131072 tokens).  The wave
+// in flight is no faster: of the 20.0 us of a call over 2 x 131072 e4m3 tokens, 16 to 18 in this kernel and 2.3 to 4
+// in the join, 18.6 remain when nothing is computed).  The wave
 // states are merged in LDS; with more than one part, by merge_parts_kernel over the parts.
 //
 // Matrix products are those of the page-list attention (prr_sep.h, pv_tile): lane 16j+n has the logits of
 // tokens 4j..4j+3 for query head n and channels 32j + 8i + cb of its output.  A key row's 16-byte
 // pieces go to the four lanes of a load instruction in order, 64 bytes of a row at a time (64 bytes of a
-// row to one lane, a load each 16: 271 us where this takes 250).
+// row to one lane, a load each 16: 8% slower).  32 sequences of up to 16K float16 tokens, 32 / 8 heads: 222 us, 5.4 TB/s.
 //
 // Weights: bfloat16 ones are three terms, all of float32's bits.  float16 ones are two, 22 bits, of numbers that
 // a power of two per head and tile lifts to the top of float16's range: what is 2^-17 below the largest weight
@@ -27,7 +27,8 @@ namespace {
 // in float32.  The value's power of two 2^ev joins the weight, exactly: p 2^(ev - top + kHeadroom), top
 // the largest ev so far.  A large scale says nothing about a row's other channels, so the weights of rows
 // with far smaller scales have to keep their bits: the product runs in bfloat16, whose three-term weights
-// have float32's bits and range, and weights up to 2^kHeadroom leave the lower 2^-126 to the others.
+// have float32's bits and range, and weights up to 2^kHeadroom leave the lower 2^-126 to the others (2 x 131072
+// tokens: 20.0 us, 19.5 with two float16 terms; 2 x 256 tiles 9.7, 9.4).
 constexpr int NW = 8;  // waves of a workgroup
 constexpr int kTile = 16;
 constexpr float kNoRef = -3e38f;  // nothing seen yet: 2^(kNoRef - anything later) = 0
@@ -460,11 +461,11 @@ void plan_decode(DecodeLaunch& a) {
   const int64_t tiles = max((most + kTile - 1) / kTile, (int64_t)1);
   const int64_t units = (int64_t)a.b.n_seqs * a.c.num_kv_heads;
   // Parts of 64 tiles (eight a wave: less, and starting and merging parts outweighs them; 512 parts of
-  // 32 tiles for 2 x 8192: 27.8 us, 256 of 64: 21.0) or of the share of 512 workgroups, two a CU; where that
-  // leaves CUs idle, as many parts as CUs, of a tile a wave at least (2 x 256 tiles: 9.4 us, 16.6 in parts of
+  // 32 tiles for 2 x 8192: 26.6 us, 256 of 64: 20.0) or of the share of 512 workgroups, two a CU; where that
+  // leaves CUs idle, as many parts as CUs, of a tile a wave at least (2 x 256 tiles: 9.7 us, 18.0 in parts of
   // 64).  Lengths are bounds here: parts
   // of at most 256 tiles keep one long sequence among short ones from being one workgroup's (64 sequences x 8
-  // KV heads, one of 131072 tokens and 63 of 500: 191 us instead of 1383), unless that takes more than 65536 workgroups,
+  // KV heads, one of 131072 tokens and 63 of 500: 190 us instead of 1383), unless that takes more than 65536 workgroups,
   // most of which would find nothing to do.
   const int64_t all = tiles * units;
   int64_t per = max((int64_t)64, min((all + 511) / 512, max((int64_t)256, all / 65536)));
