@@ -283,15 +283,16 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
     }
   }
 
-  // An infinite value meets weight terms of 0 and of the other sign and comes out as NaN.  Where there is a NaN the
-  // channel is the sum of its values that are not finite, whatever their weights.
+  const float l = sum_rows(st.l);
+  // An infinite value meets weight terms of 0 and of the other sign and comes out as NaN.  Where there is a NaN (and
+  // the weights are none) the channel is the sum of its values that are not finite, whatever their weights.
   if constexpr (!E4M3) {
     bool odd = false;
 #pragma unroll
     for (int cb = 0; cb < 8; ++cb)
 #pragma unroll
       for (int i = 0; i < 4; ++i) odd |= st.acc[cb][i] != st.acc[cb][i];
-    if (__any(odd)) {
+    if (__any(odd && l == l)) {
       f32x4_t sum[8];
 #pragma unroll
       for (int cb = 0; cb < 8; ++cb) sum[cb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -320,7 +321,6 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
   }
 
   // the wave's state, normalised
-  const float l = sum_rows(st.l);
   const float norm = l > 0.0f || l != l ? 1.0f / l : 0.0f;
   if constexpr (E4M3) {
     const int by = st.top - 127 - kHeadroom;

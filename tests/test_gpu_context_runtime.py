@@ -255,3 +255,22 @@ def test_captured_layer_calls_need_a_batch():
         want = st.cache().attend(R.Batch(DEV, [1], [t], max_kv=64), qbuf)
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip([out[0], *out[2:]], [want[0], *want[2:]]))
+
+
+@pytest.mark.gpu
+def test_the_default_stream_by_its_address():
+    """Calls of several parts on stream 0, given as a number, as a stream and not at all, from another current stream too."""
+    from paper_2606_30389_amd import runtime as R
+    pc = R.PathConfig(num_q_heads=16, num_kv_heads=1, page_size=16, num_tokens=20000, k_select=1)
+    cache = R.PagedCache(pc, DEV, k=rand(1, 1250, 16, S.D, seed=20), v=rand(1, 1250, 16, S.D, seed=21))
+    q, b, one = rand(8, 16, S.D, seed=22), R.Batch(DEV, [8], [20000]), R.Batch(DEV, [1], [20000])
+    want = cache.prompt(b, q), cache.attend(one, q[:1])
+    default, other = torch.cuda.default_stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for current in (default, other):
+        for given in (None, 0, default, other, other.cuda_stream):
+            with torch.cuda.stream(current):
+                got = cache.prompt(b, q, stream=given), cache.attend(one, q[:1], stream=given)
+                assert torch.cuda.current_stream() == current
+            torch.cuda.synchronize()
+            assert all(torch.equal(x, y) for g, w in zip(got, want) for x, y in zip(g, w))
