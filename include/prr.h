@@ -358,7 +358,7 @@ prr_status prr_rope_append(const prr_dims* dims, const prr_batch* batch, const v
  *                [0, max_pages), are left as they were
  *   num_tokens   >= 1; 0 <= page_begin <= page_end <= ceil(num_tokens / page_size)
  * Exact but for numbers below the 16-bit type's smallest normal one, which are rounded to
- * nearest. */
+ * nearest, and beyond its largest (prr_rope_append stores none), which become infinite. */
 prr_status prr_cache_read(const prr_dims* dims, const void* k_codes, const void* v_codes, const uint8_t* k_scale,
                           const uint8_t* v_scale, const int32_t* page_table, int32_t num_tokens, int32_t page_begin,
                           int32_t page_end, void* k_out, void* v_out, hipStream_t stream);
