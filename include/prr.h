@@ -12,7 +12,10 @@
  *
  * Around it, for one or many sequences: prr_rope_append writes new tokens into the paged cache
  * with their rotary positions (16 bits or e4m3), prr_prompt_attn attends prompts, prr_decode_attn
- * whole caches, prr_cache_read gives e4m3 pages back in 16 bits.
+ * whole caches, prr_cache_read gives e4m3 pages back in 16 bits.  prr_prompt_attn_shaped and
+ * prr_decode_attn_shaped do the same with capped, biased and masked scores.  A cache is made
+ * smaller by prr_key_mass (the attention weight that each token received), prr_keep_tokens (which
+ * stay) and prr_cache_compact (their rows to their new places).
  *
  * Citations name sections, equations and the appendix of "Predict, Reuse, and
  * Repair: Accelerating Dynamic Sparse Attention for Long-Context LLM Decoding".
@@ -396,6 +399,106 @@ prr_status prr_decode_attn(const prr_dims* dims, const prr_batch* batch, const v
                            const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
                            const int32_t* pages, const int32_t* page_count, int32_t cap, float* out_o32, void* out_o,
                            float* out_m, float* out_l, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------------
+ * Scores with a shape: a cap, a bias by distance, windows, documents, prefixes.
+ * --------------------------------------------------------------------------------- */
+
+/* What is done to the score z = q.k/sqrt(head_dim) of the token at position p (row r of the
+ * packed tensors) and the key at position j of sequence s, in this order:
+ *   cap      z <- cap tanh(z / cap); 0 = none, otherwise in [2^-10, 2^20]
+ *   slopes   device [Hq] float32: z <- z - slopes[head] |p - j|, or NULL
+ * and which keys the token sees: lo <= j < hi with
+ *   lo = max(0, p - window + 1, first[r])      hi = min(kv_len, max(p + 1, prefix[s]))
+ *   window   keys that a token sees back from itself, itself included; 0 = all
+ *   first    device [total_q] int32, e.g. where the token's document begins, or NULL
+ *   prefix   device [n_seqs] int32: the first so many tokens are seen by every token of the
+ *            sequence (as far as lo allows), or NULL
+ * Device values may be anything: they are cut to the sequence.  A token with a negative position
+ * sees no key, one that sees no key gets the empty state.  Positions are places in the cache.  The statistic m is the
+ * maximum of z as it is after cap and bias.  NULL in place of a shape, and one with nothing set, is the plain call. */
+typedef struct {
+  float cap;
+  int32_t window;
+  const float* slopes;
+  const int32_t* first;
+  const int32_t* prefix;
+} prr_shape;
+
+/* prr_prompt_attn with a shape; arguments, results and workspace as there.  Pages that no token of the
+ * call sees need no valid entry in the page table. */
+size_t prr_prompt_shaped_workspace_size(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape);
+prr_status prr_prompt_attn_shaped(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape, const void* q,
+                                  const void* k_cache, const void* v_cache, void* out_o, float* out_m, float* out_l,
+                                  void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* prr_decode_attn with a shape; the same.  With lists, a token attends what it sees of the listed pages. */
+size_t prr_decode_shaped_workspace_size(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape,
+                                        int32_t kv_kind, int32_t cap);
+prr_status prr_decode_attn_shaped(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape, const void* q,
+                                  int32_t kv_kind, const void* k_cache, const void* v_cache, const uint8_t* k_scale,
+                                  const uint8_t* v_scale, const int32_t* pages, const int32_t* page_count, int32_t cap,
+                                  float* out_o32, void* out_o, float* out_m, float* out_l, void* workspace,
+                                  size_t ws_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------------
+ * Eviction: a smaller cache of the tokens that received the most attention.
+ * --------------------------------------------------------------------------------- */
+
+/* The attention weight that cached tokens received from new tokens, added to what they had:
+ *   mass_out[h][j] = decay mass_in[h][j] + sum over the tokens and the query heads of KV head h of exp(z - m) / l
+ * for every token j < kv_len of every sequence (0 where none of the tokens sees j).
+ *   shape        of the scores z, as in the attention that gave m and l, or NULL: causal, plain
+ *   q            device [total_q][Hq][128] dtype
+ *   kv_kind, k_cache, k_scale  the keys (scales: E4M3 only)
+ *   m, l         device [total_q][Hq] float32, as prr_prompt_attn, prr_decode_attn or prr_repair gave them.  A token
+ *                with l = 0 gives no weight
+ *   last         only the last so many new tokens of a sequence count; 0 = all
+ *   pages, page_count, cap  as for prr_decode_attn (one token per sequence then, cu_q NULL): only tokens of
+ *                listed pages are written; or NULL
+ *   mass_in      device [Hkv][max_pages][page_size] float32, or NULL = 0 (decay is not used then)
+ *   mass_out     the same, out; may be mass_in.  Laid out as the cache is: a token's mass lies where its rows lie
+ * Sums are float32 in a fixed order: the same call gives the same bits.  List and table entries out of range are
+ * skipped.  Workspace: prr_mass_workspace_size bytes (cap 0 = no lists), 256-byte aligned, contents of no account
+ * before and after (NULL if that is 0). */
+size_t prr_mass_workspace_size(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape, int32_t kv_kind,
+                               int32_t last, int32_t cap);
+prr_status prr_key_mass(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape, const void* q, int32_t kv_kind,
+                        const void* k_cache, const uint8_t* k_scale, const float* m, const float* l, int32_t last,
+                        const int32_t* pages, const int32_t* page_count, int32_t cap, const float* mass_in, float decay,
+                        float* mass_out, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Which tokens stay: of every sequence and KV head min(budget, kv_len), the first `sink` and the last `recent` among
+ * them, the others those of the largest mass (equal ones: the lower position; NaN below everything).
+ *   batch        its kv_len and page table (the new tokens do not matter)
+ *   mass         device [Hkv][max_pages][page_size] float32, 16-byte aligned
+ *   budget       >= 1; sink, recent >= 0, sink + recent <= budget
+ *   keep         device [n_seqs][Hkv][budget] int32 out: positions, ascending; entries behind the kept ones are left as
+ *                they were
+ *   kept_len     device [n_seqs] int32 out: min(budget, kv_len)
+ * A token whose page-table entry is out of range has mass NaN.  Workspace: prr_keep_workspace_size bytes, as above. */
+size_t prr_keep_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t budget);
+prr_status prr_keep_tokens(const prr_dims* dims, const prr_batch* batch, const float* mass, int32_t budget, int32_t sink,
+                           int32_t recent, int32_t* keep, int32_t* kept_len, void* workspace, size_t ws_bytes,
+                           hipStream_t stream);
+
+/* Kept tokens to the beginning of a cache: place i of sequence s and KV head h takes what position keep[s][h][i] holds, for
+ * i < min(kept_len, budget, kv_len): keys, values, scales and mass.
+ *   keep, kept_len, budget  as prr_keep_tokens gives them (any order of positions will do)
+ *   kv_kind, k_cache, v_cache, k_scale, v_scale  the cache, in and out
+ *   mass         device [Hkv][max_pages][page_size] float32 in and out, or NULL
+ *   dst_table    device [n_seqs][dst_stride] int32: the pages of the places, none of which may be a page that a sequence
+ *                of the batch has; or NULL = the sequences' own pages (in place, none of which two sequences may share)
+ *   dst_stride   >= ceil(min(budget, max_kv) / page_size) with dst_table
+ * What is not such a place is left as it was.  Positions outside [0, kv_len) and table entries out of range are skipped.
+ * The tokens are in their order still, but at other positions: prr_rope_append's `positions` gives later tokens the
+ * rotation of their true ones.  Workspace: prr_compact_workspace_size bytes in place, none otherwise; as above. */
+size_t prr_compact_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t kv_kind, int32_t budget,
+                                  int32_t in_place);
+prr_status prr_cache_compact(const prr_dims* dims, const prr_batch* batch, const int32_t* keep, const int32_t* kept_len,
+                             int32_t budget, int32_t kv_kind, void* k_cache, void* v_cache, uint8_t* k_scale,
+                             uint8_t* v_scale, float* mass, const int32_t* dst_table, int32_t dst_stride, void* workspace,
+                             size_t ws_bytes, hipStream_t stream);
 
 /* ---------------------------------------------------------------------------------
  * Decode-step runtime: one token over a stack of layers, launched natively.

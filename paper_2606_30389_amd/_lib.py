@@ -59,6 +59,9 @@ EXPORTED = (
     "prr_read_stream", "prr_stream_chain",
     "prr_rope_freqs", "prr_rope_append", "prr_cache_read", "prr_prompt_workspace_size", "prr_prompt_attn",
     "prr_decode_workspace_size", "prr_decode_attn",
+    "prr_prompt_shaped_workspace_size", "prr_prompt_attn_shaped", "prr_decode_shaped_workspace_size", "prr_decode_attn_shaped",
+    "prr_mass_workspace_size", "prr_key_mass", "prr_keep_workspace_size", "prr_keep_tokens", "prr_compact_workspace_size",
+    "prr_cache_compact",
 )
 
 
@@ -76,6 +79,11 @@ class prr_dims(ctypes.Structure):
 class prr_batch(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int32) for name in ("n_seqs", "total_q", "max_q", "max_kv", "table_stride")] + [
         ("cu_q", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
+class prr_shape(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p), ("first", ctypes.c_void_p),
+                ("prefix", ctypes.c_void_p)]
 
 
 class prr_layer_io(ctypes.Structure):
@@ -112,6 +120,7 @@ _F = ctypes.c_float
 _S = ctypes.c_size_t
 _DIMS = ctypes.POINTER(prr_dims)
 _BATCH = ctypes.POINTER(prr_batch)
+_SHAPE = ctypes.POINTER(prr_shape)
 _L = ctypes.c_int64
 _D = ctypes.c_double
 
@@ -144,6 +153,16 @@ _SIGS = {
     "prr_prompt_attn": (_I, [_DIMS, _BATCH, _P, _P, _P, _P, _P, _P, _P, _S, _P]),
     "prr_decode_workspace_size": (_S, [_DIMS, _BATCH, _I, _I]),
     "prr_decode_attn": (_I, [_DIMS, _BATCH, _P, _I, _P, _P, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _S, _P]),
+    "prr_prompt_shaped_workspace_size": (_S, [_DIMS, _BATCH, _SHAPE]),
+    "prr_prompt_attn_shaped": (_I, [_DIMS, _BATCH, _SHAPE, _P, _P, _P, _P, _P, _P, _P, _S, _P]),
+    "prr_decode_shaped_workspace_size": (_S, [_DIMS, _BATCH, _SHAPE, _I, _I]),
+    "prr_decode_attn_shaped": (_I, [_DIMS, _BATCH, _SHAPE, _P, _I, _P, _P, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _S, _P]),
+    "prr_mass_workspace_size": (_S, [_DIMS, _BATCH, _SHAPE, _I, _I, _I]),
+    "prr_key_mass": (_I, [_DIMS, _BATCH, _SHAPE, _P, _I, _P, _P, _P, _P, _I, _P, _P, _I, _P, _F, _P, _P, _S, _P]),
+    "prr_keep_workspace_size": (_S, [_DIMS, _BATCH, _I]),
+    "prr_keep_tokens": (_I, [_DIMS, _BATCH, _P, _I, _I, _I, _P, _P, _P, _S, _P]),
+    "prr_compact_workspace_size": (_S, [_DIMS, _BATCH, _I, _I, _I]),
+    "prr_cache_compact": (_I, [_DIMS, _BATCH, _P, _P, _I, _I, _P, _P, _P, _P, _P, _P, _I, _P, _S, _P]),
     "prr_pick_delta": (_I, [_P, _P, _P, _P, _I, _I, _I, _P, _P, _P]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -384,6 +403,68 @@ def prr_decode_attn(dims, batch, q, kv_kind, k_cache, v_cache, k_scale, v_scale,
     _on_device(_lib.prr_decode_attn, q, stream, ctypes.byref(dims), ctypes.byref(batch), _ptr(q), kv_kind, _ptr(k_cache),
                _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(pages), _ptr(page_count), cap, _ptr(out_o32),
                _ptr(out_o), _ptr(out_m), _ptr(out_l), _ptr(workspace), ws_bytes)
+
+
+def make_shape(cap=0.0, slopes=None, window=0, prefix=None, first=None):
+    """A prr_shape; it keeps the tensors that it points to."""
+    sh = prr_shape(cap, window, _ptr(slopes), _ptr(first), _ptr(prefix))
+    sh.tensors = (slopes, first, prefix)
+    return sh
+
+
+def _shape(shape):
+    return None if shape is None else ctypes.byref(shape)
+
+
+def prr_prompt_shaped_workspace_size(dims, batch, shape) -> int:
+    return int(_lib.prr_prompt_shaped_workspace_size(ctypes.byref(dims), ctypes.byref(batch), _shape(shape)))
+
+
+def prr_prompt_attn_shaped(dims, batch, shape, q, k_cache, v_cache, out_o, out_m, out_l, workspace, ws_bytes, stream=None):
+    _on_device(_lib.prr_prompt_attn_shaped, q, stream, ctypes.byref(dims), ctypes.byref(batch), _shape(shape), _ptr(q),
+               _ptr(k_cache), _ptr(v_cache), _ptr(out_o), _ptr(out_m), _ptr(out_l), _ptr(workspace), ws_bytes)
+
+
+def prr_decode_shaped_workspace_size(dims, batch, shape, kv_kind, cap=0) -> int:
+    return int(_lib.prr_decode_shaped_workspace_size(ctypes.byref(dims), ctypes.byref(batch), _shape(shape), kv_kind, cap))
+
+
+def prr_decode_attn_shaped(dims, batch, shape, q, kv_kind, k_cache, v_cache, k_scale, v_scale, pages, page_count, cap, out_o32,
+                           out_o, out_m, out_l, workspace, ws_bytes, stream=None):
+    _on_device(_lib.prr_decode_attn_shaped, q, stream, ctypes.byref(dims), ctypes.byref(batch), _shape(shape), _ptr(q), kv_kind,
+               _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(pages), _ptr(page_count), cap, _ptr(out_o32),
+               _ptr(out_o), _ptr(out_m), _ptr(out_l), _ptr(workspace), ws_bytes)
+
+
+def prr_mass_workspace_size(dims, batch, shape, kv_kind, last=0, cap=0) -> int:
+    return int(_lib.prr_mass_workspace_size(ctypes.byref(dims), ctypes.byref(batch), _shape(shape), kv_kind, last, cap))
+
+
+def prr_key_mass(dims, batch, shape, q, kv_kind, k_cache, k_scale, m, l, last, pages, page_count, cap, mass_in, decay, mass_out,
+                 workspace, ws_bytes, stream=None):
+    _on_device(_lib.prr_key_mass, q, stream, ctypes.byref(dims), ctypes.byref(batch), _shape(shape), _ptr(q), kv_kind,
+               _ptr(k_cache), _ptr(k_scale), _ptr(m), _ptr(l), last, _ptr(pages), _ptr(page_count), cap, _ptr(mass_in), decay,
+               _ptr(mass_out), _ptr(workspace), ws_bytes)
+
+
+def prr_keep_workspace_size(dims, batch, budget) -> int:
+    return int(_lib.prr_keep_workspace_size(ctypes.byref(dims), ctypes.byref(batch), budget))
+
+
+def prr_keep_tokens(dims, batch, mass, budget, sink, recent, keep, kept_len, workspace, ws_bytes, stream=None):
+    _on_device(_lib.prr_keep_tokens, mass, stream, ctypes.byref(dims), ctypes.byref(batch), _ptr(mass), budget, sink, recent,
+               _ptr(keep), _ptr(kept_len), _ptr(workspace), ws_bytes)
+
+
+def prr_compact_workspace_size(dims, batch, kv_kind, budget, in_place=True) -> int:
+    return int(_lib.prr_compact_workspace_size(ctypes.byref(dims), ctypes.byref(batch), kv_kind, budget, int(bool(in_place))))
+
+
+def prr_cache_compact(dims, batch, keep, kept_len, budget, kv_kind, k_cache, v_cache, k_scale, v_scale, mass, dst_table=None,
+                      dst_stride=0, workspace=None, ws_bytes=0, stream=None):
+    _on_device(_lib.prr_cache_compact, keep, stream, ctypes.byref(dims), ctypes.byref(batch), _ptr(keep), _ptr(kept_len), budget,
+               kv_kind, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale), _ptr(mass), _ptr(dst_table), dst_stride,
+               _ptr(workspace), ws_bytes)
 
 
 def prr_empty_launch(grid, threads, stream=None):

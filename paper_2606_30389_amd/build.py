@@ -15,6 +15,8 @@ ROOT = os.path.dirname(HERE)
 SOURCES = ["csrc/prr_kernels.hip", "csrc/prr_sep_bf16.hip", "csrc/prr_sep_f16.hip", "csrc/prr_fused_bf16.hip",
            "csrc/prr_fused_f16.hip", "csrc/prr_fused_p64.hip", "csrc/prr_api.cpp", "csrc/prr_calibrate.cpp", "csrc/prr_budget.cpp",
            "csrc/prr_noalloc.hip", "csrc/prr_rope.hip", "csrc/prr_prompt.hip", "csrc/prr_decode.hip",
+           "csrc/prr_shaped_prompt_bf16.hip", "csrc/prr_shaped_prompt_f16.hip", "csrc/prr_shaped_decode_bf16.hip",
+           "csrc/prr_shaped_decode_f16.hip", "csrc/prr_mass_bf16.hip", "csrc/prr_mass_f16.hip", "csrc/prr_keep.hip",
            "csrc/prr_context.cpp"]
 OUT = os.path.join(HERE, "libprr.so")
 OBJ_DIR = os.path.join(ROOT, "_build", "obj")

@@ -81,6 +81,13 @@ prr_status check_kind(int32_t kind) {
   return PRR_OK;
 }
 
+void cache_shape(const prr_dims* d, prr::CacheArgs& c) {
+  c.num_kv_heads = d->num_kv_heads;
+  c.max_pages = d->max_pages;
+  c.page_size = d->page_size;
+  c.page_shift = log2_of(d->page_size);
+}
+
 prr_status check_cache(const prr_dims* d, int32_t kind, const void* k, const void* v, const uint8_t* ks,
                        const uint8_t* vs, prr::CacheArgs& c) {
   PRR_TRY(check_kind(kind));
@@ -94,10 +101,7 @@ prr_status check_cache(const prr_dims* d, int32_t kind, const void* k, const voi
   c.v = const_cast<void*>(v);
   c.k_scale = const_cast<uint8_t*>(ks);
   c.v_scale = const_cast<uint8_t*>(vs);
-  c.num_kv_heads = d->num_kv_heads;
-  c.max_pages = d->max_pages;
-  c.page_size = d->page_size;
-  c.page_shift = log2_of(d->page_size);
+  cache_shape(d, c);
   return PRR_OK;
 }
 
@@ -122,10 +126,38 @@ size_t parts_bytes(int64_t rows, int nsplit) {
   return ((size_t)rows * nsplit * (128 + 2) * 4 + 255) / 256 * 256;
 }
 
-prr_status plan(const prr_dims* d, const prr_batch* b, prr::PromptLaunch& a) {
+// The shape of a call's scores: its device arguments, and the bits of a kernel's instance (0: NULL, or nothing in it).
+prr_status check_shape(const prr_shape* sh, prr::ShapeArgs& a, int& bits) {
+  memset(&a, 0, sizeof(a));
+  bits = 0;
+  if (!sh) return PRR_OK;
+  if (sh->cap != 0.0f && !(sh->cap >= 0x1p-10f && sh->cap <= 0x1p20f))
+    return api_fail(PRR_ERR_INVALID_ARG, "cap %g is not 0 or in [2^-10, 2^20]", sh->cap);
+  if (sh->window < 0 || sh->window > kMaxTokens)
+    return api_fail(PRR_ERR_INVALID_ARG, "window %d outside [0, %d]", sh->window, kMaxTokens);
+  if (sh->slopes) PRR_TRY(prr::api_check_ptr(sh->slopes, "slopes", 4));
+  if (sh->prefix) PRR_TRY(prr::api_check_ptr(sh->prefix, "prefix", 4));
+  if (sh->first) PRR_TRY(prr::api_check_ptr(sh->first, "first", 4));
+  a.slopes = sh->slopes;
+  a.prefix = sh->prefix;
+  a.first = sh->first;
+  a.window = sh->window;
+  if (sh->cap != 0.0f) {
+    a.cap = (float)(sh->cap * 11.313708498984761);
+    a.inv = 1.0f / a.cap;
+    a.small = 0.5f * a.cap;
+    bits |= prr::kShapeCap;
+  }
+  if (sh->slopes) bits |= prr::kShapeSlopes;
+  if (bits || sh->window || sh->prefix || sh->first) bits |= prr::kShapeSpan;
+  return PRR_OK;
+}
+
+prr_status plan(const prr_dims* d, const prr_batch* b, const prr_shape* sh, prr::PromptLaunch& a) {
   PRR_TRY(check_heads(d));
   PRR_TRY(check_batch(d, b));
   memset(&a, 0, sizeof(a));
+  PRR_TRY(check_shape(sh, a.sh, a.shape));
   a.b = batch_args(b);
   a.num_kv_heads = d->num_kv_heads;
   a.group = d->num_q_heads / d->num_kv_heads;
@@ -143,7 +175,7 @@ prr_status plan(const prr_dims* d, const prr_batch* b, prr::PromptLaunch& a) {
   return PRR_OK;
 }
 
-prr_status plan(const prr_dims* d, const prr_batch* b, int32_t kind, int32_t cap, prr::DecodeLaunch& a) {
+prr_status plan(const prr_dims* d, const prr_batch* b, const prr_shape* sh, int32_t kind, int32_t cap, prr::DecodeLaunch& a) {
   PRR_TRY(check_heads(d));
   PRR_TRY(check_batch(d, b));
   PRR_TRY(check_kind(kind));
@@ -151,16 +183,76 @@ prr_status plan(const prr_dims* d, const prr_batch* b, int32_t kind, int32_t cap
   if (cap < 0 || cap > kMaxList || (int64_t)cap * d->page_size > kMaxTokens)
     return api_fail(PRR_ERR_INVALID_ARG, "cap %d outside [0, %d]", cap, std::min(kMaxList, kMaxTokens / d->page_size));
   memset(&a, 0, sizeof(a));
+  PRR_TRY(check_shape(sh, a.sh, a.shape));
   a.b = batch_args(b);
-  a.c.num_kv_heads = d->num_kv_heads;
-  a.c.max_pages = d->max_pages;
-  a.c.page_size = d->page_size;
-  a.c.page_shift = log2_of(d->page_size);
+  cache_shape(d, a.c);
   a.group = d->num_q_heads / d->num_kv_heads;
   a.cap = cap;
   a.bf16 = d->dtype == PRR_BF16;
   a.e4m3 = kind == PRR_KV_E4M3;
   prr::plan_decode(a);
+  return PRR_OK;
+}
+
+prr_status plan(const prr_dims* d, const prr_batch* b, const prr_shape* sh, int32_t kind, int32_t last, int32_t cap,
+                prr::MassLaunch& a) {
+  PRR_TRY(check_heads(d));
+  PRR_TRY(check_batch(d, b));
+  PRR_TRY(check_kind(kind));
+  if (last < 0) return api_fail(PRR_ERR_INVALID_ARG, "last %d < 0", last);
+  if (cap < 0 || cap > kMaxList || (int64_t)cap * d->page_size > kMaxTokens)
+    return api_fail(PRR_ERR_INVALID_ARG, "cap %d outside [0, %d]", cap, std::min(kMaxList, kMaxTokens / d->page_size));
+  memset(&a, 0, sizeof(a));
+  PRR_TRY(check_shape(sh, a.sh, a.shape));
+  a.b = batch_args(b);
+  cache_shape(d, a.c);
+  a.group = d->num_q_heads / d->num_kv_heads;
+  a.cap = cap;
+  a.last = last;
+  a.bf16 = d->dtype == PRR_BF16;
+  a.e4m3 = kind == PRR_KV_E4M3;
+  prr::plan_mass(a);
+  return PRR_OK;
+}
+
+size_t mass_bytes(const prr::MassLaunch& a) {
+  if (a.nsplit <= 1) return 0;
+  return ((size_t)a.nsplit * a.b.n_seqs * a.c.num_kv_heads * a.part_keys * 4 + 255) / 256 * 256;
+}
+
+prr_status plan(const prr_dims* d, const prr_batch* b, int32_t budget, int32_t sink, int32_t recent, prr::KeepLaunch& a) {
+  PRR_TRY(check_heads(d));
+  PRR_TRY(check_batch(d, b));
+  if (budget < 1 || budget > kMaxTokens) return api_fail(PRR_ERR_INVALID_ARG, "budget %d outside [1, %d]", budget, kMaxTokens);
+  if (sink < 0 || recent < 0 || (int64_t)sink + recent > budget)
+    return api_fail(PRR_ERR_INVALID_ARG, "sink %d and recent %d: negative, or more than the budget %d", sink, recent, budget);
+  memset(&a, 0, sizeof(a));
+  a.b = batch_args(b);
+  a.num_kv_heads = d->num_kv_heads;
+  a.max_pages = d->max_pages;
+  a.page_size = d->page_size;
+  a.page_shift = log2_of(d->page_size);
+  a.budget = budget;
+  a.sink = sink;
+  a.recent = recent;
+  prr::plan_keep(a);
+  return PRR_OK;
+}
+
+size_t keep_bytes(const prr::KeepLaunch& a) {
+  return a.chunks == 1 ? 0 : (size_t)a.b.n_seqs * a.num_kv_heads * prr::keep_words(a) * 4;
+}
+
+prr_status plan(const prr_dims* d, const prr_batch* b, int32_t kind, int32_t budget, prr::CompactLaunch& a) {
+  PRR_TRY(check_heads(d));
+  PRR_TRY(check_batch(d, b));
+  PRR_TRY(check_kind(kind));
+  if (budget < 1 || budget > kMaxTokens) return api_fail(PRR_ERR_INVALID_ARG, "budget %d outside [1, %d]", budget, kMaxTokens);
+  memset(&a, 0, sizeof(a));
+  a.b = batch_args(b);
+  cache_shape(d, a.c);
+  a.budget = budget;
+  a.e4m3 = kind == PRR_KV_E4M3;
   return PRR_OK;
 }
 
@@ -298,16 +390,26 @@ prr_status prr_cache_read(const prr_dims* dims, const void* k_codes, const void*
 }
 
 size_t prr_prompt_workspace_size(const prr_dims* dims, const prr_batch* batch) {
+  return prr_prompt_shaped_workspace_size(dims, batch, nullptr);
+}
+
+size_t prr_prompt_shaped_workspace_size(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape) {
   prr::PromptLaunch a;
-  if (plan(dims, batch, a) != PRR_OK) return 0;
+  if (plan(dims, batch, shape, a) != PRR_OK) return 0;
   return parts_bytes(part_rows(dims, a), a.nsplit);
 }
 
 prr_status prr_prompt_attn(const prr_dims* dims, const prr_batch* batch, const void* q, const void* k_cache,
                            const void* v_cache, void* out_o, float* out_m, float* out_l, void* workspace,
                            size_t ws_bytes, hipStream_t stream) {
+  return prr_prompt_attn_shaped(dims, batch, nullptr, q, k_cache, v_cache, out_o, out_m, out_l, workspace, ws_bytes, stream);
+}
+
+prr_status prr_prompt_attn_shaped(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape, const void* q,
+                                  const void* k_cache, const void* v_cache, void* out_o, float* out_m, float* out_l,
+                                  void* workspace, size_t ws_bytes, hipStream_t stream) {
   prr::PromptLaunch a;
-  PRR_TRY(plan(dims, batch, a));
+  PRR_TRY(plan(dims, batch, shape, a));
   PRR_TRY(prr::api_check_ptr(q, "q", 16));
   PRR_TRY(prr::api_check_ptr(k_cache, "k_cache", 16));
   PRR_TRY(prr::api_check_ptr(v_cache, "v_cache", 16));
@@ -332,8 +434,13 @@ prr_status prr_prompt_attn(const prr_dims* dims, const prr_batch* batch, const v
 }
 
 size_t prr_decode_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t kv_kind, int32_t cap) {
+  return prr_decode_shaped_workspace_size(dims, batch, nullptr, kv_kind, cap);
+}
+
+size_t prr_decode_shaped_workspace_size(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape, int32_t kv_kind,
+                                        int32_t cap) {
   prr::DecodeLaunch a;
-  if (plan(dims, batch, kv_kind, cap, a) != PRR_OK) return 0;
+  if (plan(dims, batch, shape, kv_kind, cap, a) != PRR_OK) return 0;
   return parts_bytes(part_rows(dims, a), a.nsplit);
 }
 
@@ -341,10 +448,19 @@ prr_status prr_decode_attn(const prr_dims* dims, const prr_batch* batch, const v
                            const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
                            const int32_t* pages, const int32_t* page_count, int32_t cap, float* out_o32, void* out_o,
                            float* out_m, float* out_l, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  return prr_decode_attn_shaped(dims, batch, nullptr, q, kv_kind, k_cache, v_cache, k_scale, v_scale, pages, page_count, cap,
+                                out_o32, out_o, out_m, out_l, workspace, ws_bytes, stream);
+}
+
+prr_status prr_decode_attn_shaped(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape, const void* q,
+                                  int32_t kv_kind, const void* k_cache, const void* v_cache, const uint8_t* k_scale,
+                                  const uint8_t* v_scale, const int32_t* pages, const int32_t* page_count, int32_t cap,
+                                  float* out_o32, void* out_o, float* out_m, float* out_l, void* workspace, size_t ws_bytes,
+                                  hipStream_t stream) {
   if (!pages != !page_count) return api_fail(PRR_ERR_INVALID_ARG, "pages and page_count: one of the two is NULL");
   if (pages && cap < 1) return api_fail(PRR_ERR_INVALID_ARG, "cap %d < 1 with lists", cap);
   prr::DecodeLaunch a;
-  PRR_TRY(plan(dims, batch, kv_kind, pages ? cap : 0, a));
+  PRR_TRY(plan(dims, batch, shape, kv_kind, pages ? cap : 0, a));
   PRR_TRY(check_cache(dims, kv_kind, k_cache, v_cache, k_scale, v_scale, a.c));
   PRR_TRY(prr::api_check_ptr(q, "q", 16));
   if (pages) {
@@ -367,6 +483,110 @@ prr_status prr_decode_attn(const prr_dims* dims, const prr_batch* batch, const v
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = a.nsplit > 1 ? a.part_o + rows * a.nsplit * 128 : nullptr;
   return hip_status(prr::launch_decode(a, stream), "decode attention");
+}
+
+size_t prr_mass_workspace_size(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape, int32_t kv_kind,
+                               int32_t last, int32_t cap) {
+  prr::MassLaunch a;
+  if (plan(dims, batch, shape, kv_kind, last, cap, a) != PRR_OK) return 0;
+  return mass_bytes(a);
+}
+
+prr_status prr_key_mass(const prr_dims* dims, const prr_batch* batch, const prr_shape* shape, const void* q, int32_t kv_kind,
+                        const void* k_cache, const uint8_t* k_scale, const float* m, const float* l, int32_t last,
+                        const int32_t* pages, const int32_t* page_count, int32_t cap, const float* mass_in, float decay,
+                        float* mass_out, void* workspace, size_t ws_bytes, hipStream_t stream) {
+  if (!pages != !page_count) return api_fail(PRR_ERR_INVALID_ARG, "pages and page_count: one of the two is NULL");
+  if (pages && cap < 1) return api_fail(PRR_ERR_INVALID_ARG, "cap %d < 1 with lists", cap);
+  prr::MassLaunch a;
+  PRR_TRY(plan(dims, batch, shape, kv_kind, last, pages ? cap : 0, a));
+  if (pages && batch->cu_q) return api_fail(PRR_ERR_INVALID_ARG, "cu_q is set: lists are of one token per sequence");
+  PRR_TRY(prr::api_check_ptr(q, "q", 16));
+  PRR_TRY(prr::api_check_ptr(k_cache, "k_cache", 16));
+  if (kv_kind == PRR_KV_E4M3) PRR_TRY(prr::api_check_ptr(k_scale, "k_scale", 16));
+  PRR_TRY(prr::api_check_ptr(m, "m", 4));
+  PRR_TRY(prr::api_check_ptr(l, "l", 4));
+  if (pages) {
+    PRR_TRY(prr::api_check_ptr(pages, "pages", 4));
+    PRR_TRY(prr::api_check_ptr(page_count, "page_count", 4));
+  }
+  if (mass_in) PRR_TRY(prr::api_check_ptr(mass_in, "mass_in", 4));
+  if (mass_in && !isfinite(decay)) return api_fail(PRR_ERR_INVALID_ARG, "decay %g", decay);
+  PRR_TRY(prr::api_check_ptr(mass_out, "mass_out", 4));
+  PRR_TRY(check_ws(workspace, ws_bytes, mass_bytes(a)));
+  a.q = q;
+  a.c.k = const_cast<void*>(k_cache);
+  a.c.k_scale = const_cast<uint8_t*>(k_scale);
+  a.m = m;
+  a.l = l;
+  a.pages = pages;
+  a.page_count = page_count;
+  a.before = mass_in;
+  a.decay = decay;
+  a.mass = mass_out;
+  a.part = static_cast<float*>(workspace);
+  if (a.b.max_kv == 0) return api_ok();  // (no sequence has a token)
+  return hip_status(prr::launch_mass(a, stream), "key mass");
+}
+
+size_t prr_keep_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t budget) {
+  prr::KeepLaunch a;
+  if (plan(dims, batch, budget, 0, 0, a) != PRR_OK) return 0;
+  return keep_bytes(a);
+}
+
+prr_status prr_keep_tokens(const prr_dims* dims, const prr_batch* batch, const float* mass, int32_t budget, int32_t sink,
+                           int32_t recent, int32_t* keep, int32_t* kept_len, void* workspace, size_t ws_bytes,
+                           hipStream_t stream) {
+  prr::KeepLaunch a;
+  PRR_TRY(plan(dims, batch, budget, sink, recent, a));
+  PRR_TRY(prr::api_check_ptr(mass, "mass", 16));
+  PRR_TRY(prr::api_check_ptr(keep, "keep", 4));
+  PRR_TRY(prr::api_check_ptr(kept_len, "kept_len", 4));
+  PRR_TRY(check_ws(workspace, ws_bytes, keep_bytes(a)));
+  a.mass = mass;
+  a.keep = keep;
+  a.kept = kept_len;
+  a.counts = static_cast<uint32_t*>(workspace);
+  return hip_status(prr::launch_keep(a, stream), "keep tokens");
+}
+
+size_t prr_compact_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t kv_kind, int32_t budget,
+                                  int32_t in_place) {
+  prr::CompactLaunch a;
+  if (plan(dims, batch, kv_kind, budget, a) != PRR_OK) return 0;
+  return in_place ? prr::compact_stage_bytes(a) : 0;
+}
+
+prr_status prr_cache_compact(const prr_dims* dims, const prr_batch* batch, const int32_t* keep, const int32_t* kept_len,
+                             int32_t budget, int32_t kv_kind, void* k_cache, void* v_cache, uint8_t* k_scale,
+                             uint8_t* v_scale, float* mass, const int32_t* dst_table, int32_t dst_stride, void* workspace,
+                             size_t ws_bytes, hipStream_t stream) {
+  prr::CompactLaunch a;
+  PRR_TRY(plan(dims, batch, kv_kind, budget, a));
+  PRR_TRY(check_cache(dims, kv_kind, k_cache, v_cache, k_scale, v_scale, a.c));
+  PRR_TRY(prr::api_check_ptr(keep, "keep", 4));
+  PRR_TRY(prr::api_check_ptr(kept_len, "kept_len", 4));
+  if (mass) PRR_TRY(prr::api_check_ptr(mass, "mass", 4));
+  if (dst_table) {
+    PRR_TRY(prr::api_check_ptr(dst_table, "dst_table", 4));
+    if (dst_table == batch->page_table)
+      return api_fail(PRR_ERR_INVALID_ARG, "dst_table is the batch's page_table: NULL means in place");
+    const int64_t rows = std::min(budget, batch->max_kv);
+    if (dst_stride < 1 || (int64_t)dst_stride * dims->page_size < rows)
+      return api_fail(PRR_ERR_INVALID_ARG, "dst_stride %d: %lld tokens need more pages of %d", dst_stride, (long long)rows,
+                      dims->page_size);
+  } else {
+    PRR_TRY(check_ws(workspace, ws_bytes, prr::compact_stage_bytes(a)));
+  }
+  a.mass = mass;
+  a.keep = keep;
+  a.kept = kept_len;
+  a.dst_table = dst_table;
+  a.dst_stride = dst_stride;
+  a.stage = static_cast<char*>(workspace);
+  if (a.b.max_kv == 0) return api_ok();  // (no sequence has a token)
+  return hip_status(prr::launch_compact(a, stream), "cache compact");
 }
 
 }  // extern "C"

@@ -9,6 +9,7 @@
 #include "prr.h"
 #include "prr_batch.h"
 #include "prr_device.h"
+#include "prr_shape.h"
 
 namespace prr {
 
@@ -62,6 +63,8 @@ struct PromptLaunch {
   int waves;   // of a workgroup, 32 rows each
   uint32_t magic;  // divides by the group size
   bool bf16;
+  ShapeArgs sh;
+  int shape;  // bits of prr_shape.h, 0: plain causal
 };
 
 struct DecodeLaunch {
@@ -79,6 +82,53 @@ struct DecodeLaunch {
   int group, cap;
   int nsplit, tiles_per_split;  // tiles of 16 tokens
   bool bf16, e4m3;
+  ShapeArgs sh;
+  int shape;  // bits of prr_shape.h, 0: every key, plain
+};
+
+struct MassLaunch {
+  const void* q;
+  CacheArgs c;  // the keys
+  const float* m;
+  const float* l;
+  const int32_t* pages;
+  const int32_t* page_count;
+  const float* before;  // or null
+  float* mass;
+  float* part;  // [nsplit][n_seqs][Hkv][part_keys] sums of a part of the rows, nsplit > 1
+  int64_t part_keys;
+  BatchArgs b;
+  int group, cap, last;
+  float decay;
+  int blocks, key_groups, nsplit;  // a wave's blocks of 16 keys, workgroups along the keys, parts of the rows
+  uint32_t magic;
+  bool bf16, e4m3;
+  ShapeArgs sh;
+  int shape;
+};
+
+struct KeepLaunch {
+  const float* mass;
+  int32_t* keep;
+  int32_t* kept;
+  BatchArgs b;
+  uint32_t* counts;  // of prr_keep.hip, where a sequence has several chunks
+  int num_kv_heads, max_pages, page_size, page_shift;
+  int budget, sink, recent;
+  int chunks, chunk;  // workgroups of a sequence and KV head, tokens of each
+};
+
+struct CompactLaunch {
+  CacheArgs c;
+  float* mass;  // or null
+  const int32_t* keep;
+  const int32_t* kept;
+  const int32_t* dst_table;  // null: in place
+  char* stage;               // rows on their way, in place
+  BatchArgs b;
+  int budget, dst_stride;
+  int phase;  // 0: to other pages, 1: to the stage, 2: from the stage
+  bool e4m3;
 };
 
 hipError_t launch_rope_append(RopeLaunch a, hipStream_t stream);
@@ -86,7 +136,26 @@ hipError_t launch_cache_read(const CacheReadLaunch& a, hipStream_t stream);
 // how the work of a call is split (host rules, by sizes alone): sets tiles / nsplit / tiles_per_split
 void plan_prompt(PromptLaunch& a);
 void plan_decode(DecodeLaunch& a);
+void plan_mass(MassLaunch& a);
+void plan_keep(KeepLaunch& a);
+hipError_t launch_mass(const MassLaunch& a, hipStream_t stream);
+template <bool BF16>
+const void* mass_kernel_of(const MassLaunch& a);
+// words of counts of one sequence and KV head (with one chunk they are not used)
+__host__ __device__ inline int64_t keep_words(const KeepLaunch& a) {
+  return ((3 * 2048 + 1) * (int64_t)a.chunks + 4 + 63) / 64 * 64;
+}
+hipError_t launch_keep(const KeepLaunch& a, hipStream_t stream);
+// bytes of the stage of a call in place
+size_t compact_stage_bytes(const CompactLaunch& a);
+hipError_t launch_compact(const CompactLaunch& a, hipStream_t stream);
 hipError_t launch_prompt(const PromptLaunch& a, hipStream_t stream);
+// the kernel of a call with a shape
+template <bool BF16>
+const void* shaped_prompt_fn(const PromptLaunch& a);
+// the kernel of a call with a shape, or that which joins its parts
+template <bool BF16>
+const void* shaped_decode_fn(const DecodeLaunch& a, bool join);
 hipError_t launch_decode(const DecodeLaunch& a, hipStream_t stream);
 
 #ifdef __HIPCC__

@@ -11,7 +11,8 @@ prediction wait for the selection only and are off the critical path.  The seria
 baseline is score_topk followed by repair with no prediction, on one stream.
 
 Around the step, PagedCache (and a LayerState's prefill and append) writes new tokens with their rotary
-positions into the paged cache, attends prompts and whole caches, and keeps a cache in e4m3.
+positions into the paged cache, attends prompts and whole caches (with a Shape: capped, biased and masked scores),
+and keeps a cache in e4m3; weigh, keep and compact (and a LayerState's evict) make a cache smaller.
 
 All arithmetic happens in libprr.so; this module only allocates, uploads and orders.
 """
@@ -95,6 +96,25 @@ class Rope:
             raise ValueError(f"freqs: shape {tuple(self.freqs.shape)}, expected one number per pair")
         self.rot_dim, self.scale = 2 * self.freqs.numel(), float(rule if scale is None else scale)
         self.layout = L.PRR_ROPE_INTERLEAVED if interleaved else L.PRR_ROPE_HALF
+
+
+class Shape:
+    """What a layer does to its scores (prr_shape): a tanh cap, a bias that falls with the distance (slopes: float32 [heads]),
+    and which keys a token sees: a window back from it, none before its document's beginning (first: int32 [rows]), and the
+    sequence's prefix (prefix: int32 [sequences])."""
+
+    def __init__(self, cap=0.0, slopes=None, window=0, first=None, prefix=None):
+        self.slopes, self.first, self.prefix = slopes, first, prefix
+        self.native = L.make_shape(cap, slopes, window, prefix, first)
+
+    def _for(self, cache, batch):
+        """The shape for a call with this batch."""
+        for x, name, n, dtype in ((self.slopes, "slopes", cache.cfg.num_q_heads, torch.float32),
+                                  (self.first, "first", batch.total_q, torch.int32),
+                                  (self.prefix, "prefix", batch.native.n_seqs, torch.int32)):
+            if x is not None:
+                _check(x, name, (n,), dtype, cache.k.device)
+        return self.native
 
 
 class Batch:
@@ -243,12 +263,14 @@ class PagedCache:
                           stream)
         return q_out
 
-    def prompt(self, batch: Batch, q, out=None, stream=None):
-        """Causal attention of the new tokens: (o in the 16-bit type, m, l); in `out`, m and l may both be None."""
+    def prompt(self, batch: Batch, q, out=None, stream=None, shape: Optional[Shape] = None):
+        """Causal attention of the new tokens, or that of a shape: (o in the 16-bit type, m, l); in `out`, m and l may both be
+        None."""
         if self.kind != L.PRR_KV_16:
             raise ValueError("prompts attend a 16-bit cache: read() the pages back first")
         self._check_batch(batch, q)
-        nbytes = L.prr_prompt_workspace_size(self.dims, batch.native)
+        shape = None if shape is None else shape._for(self, batch)
+        nbytes = L.prr_prompt_shaped_workspace_size(self.dims, batch.native, shape)
         if out is None:
             with _stream_context(stream, self.k.device):
                 n, hq = q.shape[:2]
@@ -258,20 +280,26 @@ class PagedCache:
                 if x is None and name != "o":
                     continue  # (the call itself refuses one of m and l alone)
                 _check(x, name, ref, q.dtype if name == "o" else torch.float32, self.k.device)
-        L.prr_prompt_attn(self.dims, batch.native, q, self.k, self.v, *out, self._workspace(nbytes, stream), nbytes, stream)
+        L.prr_prompt_attn_shaped(self.dims, batch.native, shape, q, self.k, self.v, *out, self._workspace(nbytes, stream), nbytes,
+                                 stream)
         return out
 
-    def attend(self, batch: Batch, q, pages=None, counts=None, out=None, stream=None):
+    def _check_lists(self, batch, pages, counts):
+        if pages is None:
+            return 0
+        per_head, cap = (batch.native.n_seqs, self.cfg.num_kv_heads), pages.shape[-1]
+        _check(pages, "pages", (*per_head, cap), torch.int32, self.k.device)
+        _check(counts, "counts", per_head, torch.int32, self.k.device)
+        return cap
+
+    def attend(self, batch: Batch, q, pages=None, counts=None, out=None, stream=None, shape: Optional[Shape] = None):
         """Attention of one token per sequence over its whole cache, or over listed pages
-        ([sequence][KV head][cap] and [sequence][KV head]): (o float32, o in the 16-bit type, m, l);
-        in `out`, the 16-bit o may be None."""
+        ([sequence][KV head][cap] and [sequence][KV head]), or what a shape lets it see of them: (o float32, o in the 16-bit
+        type, m, l); in `out`, the 16-bit o may be None."""
         self._check_batch(batch, q)
-        cap = 0 if pages is None else pages.shape[-1]
-        if pages is not None:
-            per_head = (batch.native.n_seqs, self.cfg.num_kv_heads)
-            _check(pages, "pages", (*per_head, cap), torch.int32, self.k.device)
-            _check(counts, "counts", per_head, torch.int32, self.k.device)
-        nbytes = L.prr_decode_workspace_size(self.dims, batch.native, self.kind, cap)
+        cap = self._check_lists(batch, pages, counts)
+        shape = None if shape is None else shape._for(self, batch)
+        nbytes = L.prr_decode_shaped_workspace_size(self.dims, batch.native, shape, self.kind, cap)
         if out is None:
             with _stream_context(stream, self.k.device):
                 n, hq = q.shape[:2]
@@ -281,9 +309,74 @@ class PagedCache:
             for x, name, ref in zip(out, ("o32", "o", "m", "l"), (q.shape, q.shape, q.shape[:2], q.shape[:2]), strict=True):
                 if x is not None or name != "o":
                     _check(x, name, ref, q.dtype if name == "o" else torch.float32, self.k.device)
-        L.prr_decode_attn(self.dims, batch.native, q, self.kind, self.k, self.v, self.k_scale, self.v_scale, pages, counts, cap,
-                          *out, self._workspace(nbytes, stream), nbytes, stream)
+        L.prr_decode_attn_shaped(self.dims, batch.native, shape, q, self.kind, self.k, self.v, self.k_scale, self.v_scale, pages,
+                                 counts, cap, *out, self._workspace(nbytes, stream), nbytes, stream)
         return out
+
+    def weigh(self, batch: Batch, q, m, l, before=None, decay=1.0, last=0, pages=None, counts=None, out=None, stream=None,
+              shape: Optional[Shape] = None):
+        """The attention weight that each cached token received from the new tokens (their last `last` ones, 0 = all), whose
+        attention gave m and l, on top of decay * before: float32 [Hkv][pages][page_size], laid out as the cache.  out: a
+        given one, `before` itself among them.  With lists only tokens of listed pages are written."""
+        self._check_batch(batch, q)
+        for x, name in ((m, "m"), (l, "l")):
+            _check(x, name, q.shape[:2], torch.float32, self.k.device)
+        cap = self._check_lists(batch, pages, counts)
+        for x, name in ((before, "before"), (out, "out")):
+            if x is not None:
+                _check(x, name, self.k.shape[:3], torch.float32, self.k.device)
+        shape = None if shape is None else shape._for(self, batch)
+        nbytes = L.prr_mass_workspace_size(self.dims, batch.native, shape, self.kind, last, cap)
+        if out is None:
+            with _stream_context(stream, self.k.device):
+                out = torch.zeros(self.k.shape[:3], dtype=torch.float32, device=self.k.device)
+        L.prr_key_mass(self.dims, batch.native, shape, q, self.kind, self.k, self.k_scale, m, l, last, pages, counts, cap, before,
+                       decay, out, self._workspace(nbytes, stream), nbytes, stream)
+        return out
+
+    def keep(self, batch: Batch, mass, budget, sink=0, recent=0, out=None, stream=None):
+        """The positions of the tokens that stay in a cache of at most `budget` tokens a sequence and KV head, ascending
+        ([sequence][KV head][budget]), and how many those are ([sequence], on the device): the first `sink`, the last
+        `recent`, and those of the largest mass."""
+        self._check_batch(batch, None)
+        _check(mass, "mass", self.k.shape[:3], torch.float32, self.k.device)
+        n = batch.native.n_seqs
+        nbytes = L.prr_keep_workspace_size(self.dims, batch.native, budget)
+        if out is None:
+            if budget < 1:
+                raise ValueError(f"budget {budget} < 1")
+            with _stream_context(stream, self.k.device):
+                out = (torch.zeros(n, self.cfg.num_kv_heads, budget, dtype=torch.int32, device=self.k.device),
+                       torch.zeros(n, dtype=torch.int32, device=self.k.device))
+        else:
+            for x, name, ref in zip(out, ("keep", "kept_len"), ((n, self.cfg.num_kv_heads, budget), (n,)), strict=True):
+                _check(x, name, ref, torch.int32, self.k.device)
+        L.prr_keep_tokens(self.dims, batch.native, mass, budget, sink, recent, *out, self._workspace(nbytes, stream), nbytes, stream)
+        return out
+
+    def compact(self, batch: Batch, keep, kept_len, mass=None, dst_table=None, stream=None):
+        """The kept tokens (keep's results) to the beginnings of their sequences, on the sequences' own pages or on those of
+        dst_table ([sequence][pages]); with them their mass.  The batch's lengths are the caller's to change (kept_len)."""
+        self._check_batch(batch, None)
+        n = batch.native.n_seqs
+        _check(keep, "keep", (n, self.cfg.num_kv_heads, keep.shape[-1]), torch.int32, self.k.device)
+        _check(kept_len, "kept_len", (n,), torch.int32, self.k.device)
+        if mass is not None:
+            _check(mass, "mass", self.k.shape[:3], torch.float32, self.k.device)
+        if dst_table is not None:
+            _check(dst_table, "dst_table", (n, dst_table.shape[-1]), torch.int32, self.k.device)
+        budget = keep.shape[-1]
+        nbytes = L.prr_compact_workspace_size(self.dims, batch.native, self.kind, budget, dst_table is None)
+        L.prr_cache_compact(self.dims, batch.native, keep, kept_len, budget, self.kind, self.k, self.v, self.k_scale, self.v_scale,
+                            mass, dst_table, 0 if dst_table is None else dst_table.shape[-1], self._workspace(nbytes, stream),
+                            nbytes, stream)
+
+    def evict(self, batch: Batch, mass, budget, sink=0, recent=0, dst_table=None, stream=None):
+        """keep and compact: the cache holds at most `budget` tokens of each sequence.  Returns how many ([sequence], on the
+        device); the batch's lengths are the caller's to change."""
+        keep, kept_len = self.keep(batch, mass, budget, sink, recent, stream=stream)
+        self.compact(batch, keep, kept_len, mass, dst_table, stream)
+        return kept_len
 
     def read(self, num_tokens, page_table=None, page_begin=0, page_end=None, out=None, stream=None):
         """Pages of a sequence of an e4m3 cache in 16 bits: (k, v) [Hkv][pages][page_size][128]."""
@@ -372,26 +465,46 @@ class LayerState:
             raise ValueError(f"a batch of {batch.native.n_seqs} sequences: a layer holds one")
         return self.batch(new_tokens, stream) if batch is None else batch
 
-    def prefill(self, q, k, v, rope: Optional[Rope] = None, batch: Optional[Batch] = None, stream=None):
-        """The last len(q) of the cfg.num_tokens tokens: into the cache, their causal attention, and the metadata
-        of the pages that they touch.  q [n][Hq][128], k, v [n][Hkv][128]; returns (o, m, l).  A given batch holds
+    def prefill(self, q, k, v, rope: Optional[Rope] = None, batch: Optional[Batch] = None, stream=None,
+                shape: Optional[Shape] = None, positions=None, q_out=None):
+        """The last len(q) of the cfg.num_tokens tokens: into the cache, their causal attention (or that of a shape), and the
+        metadata of the pages that they touch.  q [n][Hq][128], k, v [n][Hkv][128]; returns (o, m, l), in a given q_out the
+        rotated queries.  positions: the tokens' true ones, after an eviction.  A given batch holds
         this one sequence, of cfg.num_tokens tokens; its rows may be more than its new tokens."""
         cfg = self.cfg
         batch = self._one(batch, q.shape[0], stream)
-        q = self.cache().append(batch, q, k, v, rope, stream=stream)
-        out = self.cache().prompt(batch, q, stream=stream)
+        q = self.cache().append(batch, q, k, v, rope, positions=positions, q_out=q_out, stream=stream)
+        out = self.cache().prompt(batch, q, stream=stream, shape=shape)
         # (rows behind the tokens, and tokens without a place, count for none)
         self.build_meta(stream, page_begin=max(0, cfg.num_tokens - q.shape[0]) // cfg.page_size)
         return out
 
-    def append(self, q, k, v, rope: Optional[Rope] = None, batch: Optional[Batch] = None, q_out=None, stream=None):
+    def append(self, q, k, v, rope: Optional[Rope] = None, batch: Optional[Batch] = None, q_out=None, stream=None,
+               positions=None):
         """One new token, the last of the cfg.num_tokens: into the cache, and its page's metadata; returns the
-        rotated query, ready for select() or a decode step.  The metadata's page is that of this moment: a captured graph
-        keeps it."""
+        rotated query, ready for select() or a decode step.  positions: the token's true one (int32 [1]), after an eviction.
+        The metadata's page is that of this moment: a captured graph keeps it."""
         cfg = self.cfg
-        q = self.cache().append(self._one(batch, 1, stream), q, k, v, rope, q_out=q_out, stream=stream)
+        q = self.cache().append(self._one(batch, 1, stream), q, k, v, rope, positions=positions, q_out=q_out, stream=stream)
         self.build_meta(stream, page_begin=(cfg.num_tokens - 1) // cfg.page_size)
         return q
+
+    def evict(self, q, m, l, budget, sink=0, recent=0, last=0, batch: Optional[Batch] = None, stream=None,
+              shape: Optional[Shape] = None):
+        """The cache with at most `budget` of the cfg.num_tokens tokens: the first `sink`, the last `recent`, and those that
+        received the most attention from the last new tokens, whose rotated queries q [n][Hq][128] and statistics m, l a
+        prefill gave.  Metadata is built anew, predictions start anew.  Returns the tokens that stay, which
+        DecodeStack.set_tokens makes the layers' length once all of them are evicted to it."""
+        cfg, cache = self.cfg, self.cache()
+        batch = self._one(batch, q.shape[0], stream)
+        mass = cache.weigh(batch, q, m, l, last=last, stream=stream, shape=shape)
+        cache.evict(batch, mass, budget, sink, recent, stream=stream)
+        kept = min(budget, cfg.num_tokens)
+        L.prr_build_page_meta(self.dims, self.k, self.page_table, kept, 0, -(-kept // cfg.page_size), self.meta, stream)
+        with _stream_context(stream, self.k.device):
+            for x in (self.init_bits, *self.pred_count):
+                x.zero_()
+        return kept
 
     # --------------------------------------------------------------- steps
     def build_meta(self, stream=None, page_begin=0, page_end=None):
