@@ -199,6 +199,7 @@ __device__ __forceinline__ uint32_t* unit_words(const KeepLaunch& a, int s, int 
 // The thread's two bins of all chunks that have tokens
 __device__ __forceinline__ void sum_bins(const uint32_t* counts, int chunks, int& c0, int& c1) {
   c0 = c1 = 0;
+#pragma unroll 16
   for (int c = 0; c < chunks; ++c) {
     const uint2 x = *reinterpret_cast<const uint2*>(counts + (int64_t)c * kBins + 2 * threadIdx.x);
     c0 += (int)x.x;
@@ -285,6 +286,7 @@ __global__ __launch_bounds__(kThreads) void keep_write_kernel(const KeepLaunch a
     tk.key = state[2] << 10 | (uint32_t)bin;
     tk.ties = rest;
     int more = 0, same = 0;
+#pragma unroll 16
     for (int x = 0; x < c; ++x) {
       const uint2 own = *reinterpret_cast<const uint2*>(last + (int64_t)x * kBins + 2 * t);
       more += (2 * t > bin ? (int)own.x : 0) + (2 * t + 1 > bin ? (int)own.y : 0);
@@ -374,13 +376,13 @@ __global__ __launch_bounds__(256) void compact_kernel(const CompactLaunch a) {
     const char* const v_src = a.phase == 2 ? stage_v : static_cast<const char*>(a.c.v);
     char* const k_dst = a.phase == 1 ? stage_k : static_cast<char*>(a.c.k);
     char* const v_dst = a.phase == 1 ? stage_v : static_cast<char*>(a.c.v);
-    uint4 k[kSteps], v[kSteps];
+    u32x4_t k[kSteps], v[kSteps];
     const int c = (t % kLanes) * 16;
 #pragma unroll
     for (int x = 0; x < kSteps; ++x) {  // (row 0 in place of one that does not move)
       const int64_t f = max(from[t / kLanes + x * (256 / kLanes)], (int64_t)0);
-      k[x] = *reinterpret_cast<const uint4*>(k_src + f * kRowBytes + c);
-      v[x] = *reinterpret_cast<const uint4*>(v_src + f * kRowBytes + c);
+      k[x] = *reinterpret_cast<const u32x4_t*>(k_src + f * kRowBytes + c);
+      v[x] = *reinterpret_cast<const u32x4_t*>(v_src + f * kRowBytes + c);
     }
     if (t < kMoveRows && from[t] >= 0) {
       const int64_t f = from[t], d = to[t];
@@ -394,8 +396,8 @@ __global__ __launch_bounds__(256) void compact_kernel(const CompactLaunch a) {
     for (int x = 0; x < kSteps; ++x) {
       const int64_t d = to[t / kLanes + x * (256 / kLanes)];
       if (d >= 0) {
-        *reinterpret_cast<uint4*>(k_dst + d * kRowBytes + c) = k[x];
-        *reinterpret_cast<uint4*>(v_dst + d * kRowBytes + c) = v[x];
+        *reinterpret_cast<u32x4_t*>(k_dst + d * kRowBytes + c) = k[x];
+        *reinterpret_cast<u32x4_t*>(v_dst + d * kRowBytes + c) = v[x];
       }
     }
   }

@@ -32,7 +32,7 @@ void plan_mass(MassLaunch& a) {
   const int64_t rows = (int64_t)(a.last ? min(a.last, a.b.max_q) : a.b.max_q) * a.group;
   const int64_t units = (int64_t)a.b.n_seqs * a.c.num_kv_heads;
   const int64_t blocks = max((keys + 15) / 16, (int64_t)1);
-  a.blocks = blocks * units >= 16 * 256 ? 4 : 1;
+  a.blocks = blocks * units >= 16 * 256 || rows >= 2048 ? 4 : 1;
   const int64_t per = 64 * a.blocks;
   int64_t groups = max((keys + per - 1) / per, (int64_t)1);
   a.part_keys = groups * per;
@@ -41,12 +41,13 @@ void plan_mass(MassLaunch& a) {
   // (a workgroup walks over several groups of keys where there are very many)
   groups = min(groups, max((int64_t)1, ((int64_t)1 << 20) / units));
   a.key_groups = (int)groups;
+  for (int i = 0; i < 5; ++i) a.k2[i] = a.sh.k[i] * kSoftmaxScale2;
   a.magic = a.group == 1 ? 0u : (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
 }
 
 hipError_t launch_mass(const MassLaunch& a, hipStream_t stream) {
   const void* f = a.bf16 ? mass_kernel_of<true>(a) : mass_kernel_of<false>(a);
-  const hipError_t e = launch_one(f, dim3(a.key_groups * a.nsplit, a.c.num_kv_heads, a.b.n_seqs), 256, stream, a);
+  const hipError_t e = launch_one(f, dim3(a.key_groups * a.nsplit * a.c.num_kv_heads, 1, a.b.n_seqs), 256, stream, a);
   if (e != hipSuccess || a.nsplit == 1) return e;
   return launch_one((const void*)mass_join_kernel, dim3((unsigned)((a.b.max_kv + 255) / 256), a.c.num_kv_heads, a.b.n_seqs), 256,
                     stream, a);

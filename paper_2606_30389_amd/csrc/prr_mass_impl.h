@@ -21,7 +21,6 @@ namespace {
 //
 // Every 32 tiles a lane's sums go to a second set, so that a sum of n rows is off by about (128 + n / 2048) 2^-24 at most.
 constexpr int kRows = 64;                 // rows of a tile
-constexpr int kPitch = kHeadDim + 8;      // elements of a row in LDS: a read of 16 bytes of 16 rows meets every bank once
 constexpr int kFlush = 32;
 
 template <bool BF16>
@@ -37,14 +36,16 @@ __device__ __forceinline__ f32x4_t mass_mfma(const u32x4_t& a, const u32x4_t& b,
 __device__ __forceinline__ int mass_over_group(int x, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)x, magic) : x; }
 
 template <bool BF16, bool E4M3, int KB, int SHAPE>
-__global__ __launch_bounds__(256) void mass_kernel(const MassLaunch a) {
-  __shared__ __align__(16) uint16_t lq[2][kRows * kPitch];
+__global__ __launch_bounds__(256, 2) void mass_kernel(const MassLaunch a) {
+  __shared__ __align__(16) uint16_t lq[2][kRows * kHeadDim];
+  __shared__ float l_total[KB][4][256];
   __shared__ float l_ref[2][kRows], l_slope[2][kRows];
   __shared__ int l_lo[2][kRows], l_hi[2][kRows], l_pos[2][kRows];
   const int t = threadIdx.x, lane = lane_id(), w = __builtin_amdgcn_readfirstlane(t / kWave);
   const int j = lane >> 4, n = lane & 15;
-  const int h = blockIdx.y, s = blockIdx.z, G = a.group;
-  const int part = (int)(blockIdx.x % a.nsplit);
+  // (the heads of a group of keys side by side: the first keys, which most rows see, of all heads begin first)
+  const int h = (int)(blockIdx.x % a.c.num_kv_heads), s = blockIdx.z, G = a.group;
+  const int step = a.nsplit * a.c.num_kv_heads;
   const Seq sq = seq_at(a.b, s);
   const int q_len = sq.q1 - sq.q0, counted = a.last ? min(a.last, q_len) : q_len;
   const int first = sq.kv - q_len;  // position of the first new token
@@ -53,7 +54,9 @@ __global__ __launch_bounds__(256) void mass_kernel(const MassLaunch a) {
   const int64_t keys = a.pages ? (int64_t)list << a.c.page_shift : sq.kv;
   const int64_t head_row = (int64_t)h * a.c.max_pages * a.c.page_size;
 
-  for (int kg = (int)(blockIdx.x / a.nsplit); (int64_t)kg * 64 * KB < keys; kg += (int)(gridDim.x / a.nsplit)) {
+  for (int kg = (int)(blockIdx.x / step); (int64_t)kg * 64 * KB < keys; kg += (int)(gridDim.x / step)) {
+    // (turned from group to group, as workgroups go to the XCDs in turn and a group's first part has the diagonal)
+    const int part = (int)((blockIdx.x / a.c.num_kv_heads + kg) % a.nsplit);
     // the wave's blocks of 16 keys: first cache row, position of the first key, keys that there are
     int64_t my_row = 0;
     int my_tok = 0, my_valid = 0;
@@ -123,14 +126,24 @@ __global__ __launch_bounds__(256) void mass_kernel(const MassLaunch a) {
     const int per = (tiles + a.nsplit - 1) / a.nsplit;
     const int t0 = min(part * per, tiles), t1 = min(t0 + per, tiles);
 
-    f32x4_t sum[KB], total[KB];
+    f32x4_t sum[KB];
 #pragma unroll
-    for (int b = 0; b < KB; ++b) sum[b] = total[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < KB; ++b) sum[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const bool flushes = t1 - t0 > kFlush;
+    if (flushes) {
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l_total[b][i][t] = 0.0f;
+    }
 
-    // thread t brings chunks t%16 of rows t/16 + 16 x, threads 0..63 what is known of row t
+    // Thread t brings 16 bytes of rows t/16 + 16 x; the place of row r's 16 bytes c is c ^ (r % 16), so that a read of the
+    // same bytes of 16 rows meets every bank once.  Threads 0..63 bring what is known of row t.  Nothing of it is looked at
+    // before the products of the tile before are done.
     u32x4_t qr[4];
-    float r_ref = 0.0f, r_slope = 0.0f;
-    int r_lo = 0, r_hi = 0, r_pos = 0;
+    float r_m = 0.0f, r_l = 0.0f, r_slope = 0.0f;
+    int r_first = 0, r_pos = 0;
+    bool r_live = false;
     const auto load = [&](int tile) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
@@ -143,22 +156,23 @@ __global__ __launch_bounds__(256) void mass_kernel(const MassLaunch a) {
         const int r = min(tile * kRows + t, rows - 1);
         const int tok = mass_over_group(r, a.magic), head = r - tok * G;
         const int64_t at = ((int64_t)(sq.q0 + i0 + tok) * a.c.num_kv_heads + h) * G + head;
-        const float m = a.m[at], l = a.l[at];
-        r_ref = l == 0.0f ? __builtin_inff() : fmaf(m, kLog2e, __builtin_amdgcn_logf(l));
+        r_m = a.m[at];
+        r_l = a.l[at];
+        r_first = a.sh.first ? a.sh.first[sq.q0 + i0 + tok] : 0;
         r_pos = first + i0 + tok;
-        const Span sp = span_of(a.sh, r_pos, sq.q0 + i0 + tok, s, sq.kv);
-        r_lo = sp.lo;
-        r_hi = tile * kRows + t < rows ? sp.hi : sp.lo;  // (rows behind the last see nothing)
+        r_live = tile * kRows + t < rows;  // (rows behind the last see nothing)
         if constexpr (SHAPE & kShapeSlopes) r_slope = a.sh.slopes[h * G + head] * kRawPerLogit;
       }
     };
     const auto store = [&](int buf) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) *reinterpret_cast<u32x4_t*>(&lq[buf][((t >> 4) + 16 * x) * kPitch + 8 * (t & 15)]) = qr[x];
+      for (int x = 0; x < 4; ++x)
+        *reinterpret_cast<u32x4_t*>(&lq[buf][((t >> 4) + 16 * x) * kHeadDim + 8 * ((t & 15) ^ ((t >> 4) & 15))]) = qr[x];
       if (t < kRows) {
-        l_ref[buf][t] = r_ref;
-        l_lo[buf][t] = r_lo;
-        l_hi[buf][t] = r_hi;
+        const Span sp = span_at(a.sh.window, r_first, prefix, r_pos, sq.kv);
+        l_ref[buf][t] = r_l == 0.0f ? __builtin_inff() : fmaf(r_m, kLog2e, __builtin_amdgcn_logf(r_l));
+        l_lo[buf][t] = sp.lo;
+        l_hi[buf][t] = r_live ? sp.hi : sp.lo;
         if constexpr (SHAPE & kShapeSlopes) {
           l_pos[buf][t] = r_pos;
           l_slope[buf][t] = r_slope;
@@ -166,15 +180,12 @@ __global__ __launch_bounds__(256) void mass_kernel(const MassLaunch a) {
       }
     };
     // 16 rows, from row 16 u of the tile in the buffer on
-    const auto products = [&](int buf, int u) {
-      const int lo = l_lo[buf][16 * u + n], hi = l_hi[buf][16 * u + n];
-      const float ref = l_ref[buf][16 * u + n];
-      if (!__any(lo < wk1 && hi > wk0 && lo < hi)) return;
-      const bool whole = run && __all(lo <= wk0 && hi >= wk1);
+    const auto products = [&](int buf, int u, auto masked) {
       u32x4_t qf[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        qf[x] = *reinterpret_cast<const u32x4_t*>(&lq[buf][(16 * u + n) * kPitch + (E4M3 ? 64 * (x >> 1) + 16 * j + 8 * (x & 1) : 32 * x + 8 * j)]);
+        qf[x] = *reinterpret_cast<const u32x4_t*>(&lq[buf][(16 * u + n) * kHeadDim + 8 * ((E4M3 ? 8 * (x >> 1) + 2 * j + (x & 1) : 4 * x + j) ^ n)]);
+      const float ref = l_ref[buf][16 * u + n];
       f32x4_t d[KB];
 #pragma unroll
       for (int b = 0; b < KB; ++b) d[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -188,18 +199,15 @@ __global__ __launch_bounds__(256) void mass_kernel(const MassLaunch a) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) d[b][i] *= ks[b][i];
       }
+      [[maybe_unused]] bool small = false;
       if constexpr (SHAPE & kShapeCap) {
         float most = 0.0f;
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
           for (int i = 0; i < 4; ++i) most = fmaxf(most, fabsf(d[b][i]));
-        if (__all(most < a.sh.small)) {
-#pragma unroll
-          for (int b = 0; b < KB; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) d[b][i] = cap_small(d[b][i], a.sh);
-        } else {
+        small = __all(most < a.sh.small);
+        if constexpr (SHAPE & kShapeSlopes) {
 #pragma unroll
           for (int b = 0; b < KB; ++b)
 #pragma unroll
@@ -216,11 +224,32 @@ __global__ __launch_bounds__(256) void mass_kernel(const MassLaunch a) {
           for (int i = 0; i < 4; ++i) d[b][i] = fmaf(-slope, fabsf(ahead + (float)i), d[b][i]);
         }
       }
+      // (the change to powers of two is in k2 where nothing comes between)
+      const auto weight = [&](float x) { return exp2_hw(fmaf(x, kSoftmaxScale2, -ref)); };
+      if constexpr (SHAPE == kShapeCap) {
+        if (small) {
 #pragma unroll
-      for (int b = 0; b < KB; ++b)
+          for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) d[b][i] = exp2_hw(fmaf(d[b][i], kSoftmaxScale2, -ref));
-      if (!whole) {
+            for (int i = 0; i < 4; ++i) d[b][i] = exp2_hw(fmaf(d[b][i], cap_ratio(d[b][i], a.k2, kSoftmaxScale2), -ref));
+        } else {
+#pragma unroll
+          for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float near = fmaf(d[b][i], cap_ratio(d[b][i], a.k2, kSoftmaxScale2), -ref);
+              const float far = fmaf(cap_large(d[b][i], a.sh), kSoftmaxScale2, -ref);
+              d[b][i] = exp2_hw(fabsf(d[b][i]) < a.sh.small ? near : far);
+            }
+        }
+      } else {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[b][i] = weight(d[b][i]);
+      }
+      if constexpr (masked.value) {
+        const int lo = l_lo[buf][16 * u + n], hi = l_hi[buf][16 * u + n];
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
           const uint32_t at = (uint32_t)(tok0[b] + 4 * j - lo), seen = (uint32_t)(hi - lo);
@@ -231,6 +260,24 @@ __global__ __launch_bounds__(256) void mass_kernel(const MassLaunch a) {
 #pragma unroll
       for (int b = 0; b < KB; ++b) sum[b] += d[b];
     };
+    // The tile in the buffer: a lane looks at a row's keys
+    const auto tile_products = [&](int buf) {
+      const int lo = l_lo[buf][lane], hi = l_hi[buf][lane];
+      const uint64_t some = __ballot(lo < wk1 && hi > wk0 && lo < hi);
+      const uint64_t whole = run ? __ballot(lo <= wk0 && hi >= wk1) : 0;
+      if (whole == ~0ull) {
+#pragma unroll
+        for (int u = 0; u < kRows / 16; ++u) products(buf, u, std::false_type{});
+      } else {
+        for (int u = 0; u < kRows / 16; ++u) {
+          if (((whole >> (16 * u)) & 0xffff) == 0xffff) {
+            products(buf, u, std::false_type{});
+          } else if ((some >> (16 * u)) & 0xffff) {
+            products(buf, u, std::true_type{});
+          }
+        }
+      }
+    };
 
     if (t0 < t1) {
       load(t0);
@@ -239,25 +286,32 @@ __global__ __launch_bounds__(256) void mass_kernel(const MassLaunch a) {
       for (int tile = t0; tile < t1; ++tile) {
         const int buf = (tile - t0) & 1;
         if (tile + 1 < t1) load(tile + 1);
-#pragma unroll
-        for (int u = 0; u < kRows / 16; ++u) products(buf, u);
+        tile_products(buf);
         if (tile + 1 < t1) store(buf ^ 1);
-        if (((tile - t0) & (kFlush - 1)) == kFlush - 1) {
+        if (flushes && ((tile - t0) & (kFlush - 1)) == kFlush - 1) {
 #pragma unroll
-          for (int b = 0; b < KB; ++b) {
-            total[b] += sum[b];
-            sum[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-          }
+          for (int b = 0; b < KB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              l_total[b][i][t] += sum[b][i];
+              sum[b][i] = 0.0f;
+            }
         }
         __syncthreads();
       }
+    }
+    if (flushes) {
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[b][i] += l_total[b][i][t];
     }
 
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
       float r[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = sum16(total[b][i] + sum[b][i]);
+      for (int i = 0; i < 4; ++i) r[i] = sum16(sum[b][i]);
       if (n < 4) {  // lane 16j+i stores key 4j+i
         const float v = n == 0 ? r[0] : n == 1 ? r[1] : n == 2 ? r[2] : r[3];
         if (a.nsplit > 1) {

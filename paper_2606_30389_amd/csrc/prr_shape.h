@@ -13,6 +13,7 @@ struct ShapeArgs {
   const int32_t* first;
   int window;
   float cap, inv, small;  // the cap in the units of q.k, 1 / cap, the logits below which cap_small holds
+  float k[5];             // cap_small's coefficients
 };
 
 // Keys [lo, hi) of a sequence of kv tokens that the token at position pos (row `row` of the packed tensors) sees; lo = hi:
@@ -20,38 +21,43 @@ struct ShapeArgs {
 struct Span {
   int lo, hi;
 };
-__device__ __forceinline__ Span span_of(const ShapeArgs& a, int pos, int row, int s, int kv) {
+// first: where the row's document begins; prefix: the tokens of the sequence's prefix
+__device__ __forceinline__ Span span_at(int window, int first, int prefix, int pos, int kv) {
   Span r;
   if (pos < 0) {
     r.lo = r.hi = 0;
     return r;
   }
-  r.lo = a.window ? max(pos - a.window + 1, 0) : 0;
-  if (a.first) r.lo = max(r.lo, a.first[row]);
-  r.hi = pos + 1;
-  if (a.prefix) r.hi = min(max(r.hi, a.prefix[s]), kv);
+  r.lo = max(window ? max(pos - window + 1, 0) : 0, first);
+  r.hi = min(max(pos + 1, prefix), kv);
   r.lo = min(r.lo, r.hi);
   return r;
 }
+__device__ __forceinline__ Span span_of(const ShapeArgs& a, int pos, int row, int s, int kv) {
+  return span_at(a.window, a.first ? a.first[row] : 0, a.prefix ? a.prefix[s] : 0, pos, kv);
+}
+
+// P of cap_small: tanh(x) / x = 1 + t0 x^2 + t1 x^4 + ...
+constexpr double kTanh[5] = {-0.3333318990018068, 0.1332911073996761, -0.05355886142021114, 0.020091970334283688, -0.005138662405571459};
+constexpr double kTanhRange = 0.7;
 
 #ifdef __HIPCC__
 
 // Logits are held as q.k: a logit's cap and slopes in that unit.
 constexpr float kRawPerLogit = 11.313708498984761f;  // sqrt(128)
 
-// cap tanh(s / cap), s in the units of q.k.  Below half the cap: s P((s / cap)^2), P the polynomial of degree 4 closest to
-// tanh(x) / x up to 1/2 (least squares with weights moved until the relative error was level): 2^-26 relative before
-// rounding, 2^-23 with it.  Seven operations where the other form needs an exponential and a reciprocal, each
-// a quarter of an operation's rate.
-__device__ __forceinline__ float cap_small(float s, const ShapeArgs& a) {
-  const float x = s * a.inv, u = x * x;
-  float p = 0.017135007306933403f;
-  p = fmaf(p, u, -0.05298607423901558f);
-  p = fmaf(p, u, 0.13324779272079468f);
-  p = fmaf(p, u, -0.3333306908607483f);
-  p = fmaf(p, u, 1.0f);
-  return s * p;
+// cap tanh(s / cap), s in the units of q.k.  Below 0.7 of the cap: s P((s / cap)^2), P the polynomial of degree 5 closest to
+// tanh(x) / x there (least squares with weights moved until the relative error was level): 2^-26 relative before
+// rounding, 2^-23 with it.  k holds P's coefficients times powers of 1 / cap^2, so that s^2 is the argument: seven operations
+// where the other form needs an exponential and a reciprocal, too, each a quarter of an operation's rate.  A tile
+// whose logits are all below takes this form alone; in one of both kinds each logit takes its own, so that no result depends
+// on the others' logits.  (Degree 4 up to 1/2 leaves more tiles of both kinds: nine packed prompts with a cap
+// of 30 and logits of standard deviation 4, 266 us.)
+__device__ __forceinline__ float cap_ratio(float s, const float (&k)[5], float one) {
+  const float u = s * s;
+  return fmaf(fmaf(fmaf(fmaf(fmaf(k[4], u, k[3]), u, k[2]), u, k[1]), u, k[0]), u, one);
 }
+__device__ __forceinline__ float cap_small(float s, const ShapeArgs& a) { return s * cap_ratio(s, a.k, 1.0f); }
 // Any s: cap (1 - 2 / (1 + e^(2 s / cap))), off by at most cap * 2^-22 (the reciprocal's and the sum's last places);
 // infinities give the cap, NaN stays NaN.
 __device__ __forceinline__ float cap_large(float s, const ShapeArgs& a) {
