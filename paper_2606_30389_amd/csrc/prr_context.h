@@ -144,7 +144,7 @@ template <bool BF16>
 const void* mass_kernel_of(const MassLaunch& a);
 // words of counts of one sequence and KV head (with one chunk they are not used)
 __host__ __device__ inline int64_t keep_words(const KeepLaunch& a) {
-  return ((3 * 2048 + 1) * (int64_t)a.chunks + 4 + 63) / 64 * 64;
+  return (2048 * (int64_t)a.chunks + 64 + 4 + 2 * (int64_t)a.chunks * a.chunk + 63) / 64 * 64;
 }
 hipError_t launch_keep(const KeepLaunch& a, hipStream_t stream);
 // bytes of the stage of a call in place

@@ -9,24 +9,29 @@ namespace {
 // the tokens of the largest mass
 // =====================================================================================
 // Of a sequence and KV head: the first `sink` and the last `recent` tokens, and of those between them the ones of the largest
-// mass, the lower position first among equals.  A mass becomes a 32-bit key of the same order; counting the keys by 11, 11
-// and 10 bits finds the key of the last token taken, and how many of that key are.  Positions come out in order: a token's
-// place is the number of taken tokens before it.
+// mass, the lower position first among equals.  A mass becomes a 32-bit key of the same order.  Counting the keys by their
+// first 11 bits finds the bin that the last token taken is in; the keys of that bin, a few hundred of 16384 where masses
+// differ, are listed and counted by the next 11 and 10 bits.  So the threshold's key is known and how many of that key
+// are taken, and positions come out in order: a token's place is the number of taken tokens before it.
 //
-// Up to 32768 tokens one workgroup does all of it, the keys in registers; the counts lie in LDS eightfold, as masses
-// share few exponents and lanes that count the same bin wait for each other.  More tokens are cut into chunks of as
-// many workgroups, a launch per step: counts of each chunk in device memory, added up by all.
+// Up to 32768 tokens one workgroup does all of it, the keys in registers.  Masses share few exponents, and lanes that
+// count the same bin wait for each other: there are eight counts of a bin, in banks of their own.  More tokens are cut into
+// chunks of as many workgroups, in three launches: counts of each chunk in device memory; their sum, by every workgroup
+// for itself, and the keys of the bin into a list; the threshold from the list, by every workgroup for itself again.
+// Bound by latency: of the 13 us of 32 sequences of up to 16384 tokens and 8 KV heads, launch and keys take 4.9, the first
+// count 2.6, the list and its counts 2.7, the places 3.  131072 tokens of 2 KV heads: 21 us (40 with three counts and a
+// launch for each).
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
-constexpr int kBins = 2048, kCopies = 8;
-constexpr int kSmall = 32768;      // tokens of one workgroup
+constexpr int kBins = 2048, kCopies = 8, kCopyPitch = kBins + 8;
+constexpr int kSmall = 32768;  // tokens of one workgroup
 constexpr int kMaxChunks = 64;
+constexpr int kListed = 8192;  // keys of a bin that are listed in LDS
 
-// Larger mass, larger key; NaN below everything
-__device__ __forceinline__ uint32_t mass_key(float f) { return f != f ? 0u : score_key(f); }
-
-__device__ __forceinline__ uint32_t bin_of(uint32_t key, int level) {
-  return level == 0 ? key >> 21 : level == 1 ? (key >> 10) & 2047u : key & 1023u;
-}
+// Larger mass, larger key; NaN below everything; tokens that are kept whatever their mass above everything
+constexpr uint32_t kAbsent = 0, kNaN = 1, kAlways = 0xffffffffu;
+__device__ __forceinline__ uint32_t mass_key(float f) { return f != f ? kNaN : score_key(f); }
+// A key that stands for a mass
+__device__ __forceinline__ bool by_mass(uint32_t key) { return key - 1 < kAlways - 1; }
 
 struct Unit {
   int kv, count, sink, end;  // tokens; kept ones; [sink, end): those chosen by their mass
@@ -39,58 +44,122 @@ __device__ __forceinline__ Unit unit_of(const KeepLaunch& a, int s) {
   u.end = u.count == u.kv ? u.kv : u.kv - a.recent;
   return u;
 }
+// Tokens that are chosen by their mass: at most as many as there are
+__device__ __forceinline__ int chosen(const Unit& u) { return u.count - u.sink - (u.kv - u.end); }
 
-// The keys of tokens [p, p + 4), p a multiple of 4 and below kv; what is behind kv, or has no page, is 0
-__device__ __forceinline__ void load_keys(const KeepLaunch& a, int s, int h, int p, int kv, uint32_t (&key)[4]) {
+// Where the masses of tokens [p, p + 4) lie, p a multiple of 4 below max_kv (-1: nowhere).  Needs no length, so that the
+// lookup does not wait for it; what is behind the length is not used.
+__device__ __forceinline__ int64_t find_keys(const KeepLaunch& a, int s, int h, int p) {
   const int phys = phys_page(a.b.page_table, a.b.table_stride, a.max_pages, s, p >> a.page_shift);
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (phys >= 0)
-    v = *reinterpret_cast<const float4*>(a.mass + (((int64_t)h * a.max_pages + phys) << a.page_shift) + (p & (a.page_size - 1)));
-  key[0] = phys >= 0 ? mass_key(v.x) : 0u;
-  key[1] = phys >= 0 ? mass_key(v.y) : 0u;
-  key[2] = phys >= 0 ? mass_key(v.z) : 0u;
-  key[3] = phys >= 0 ? mass_key(v.w) : 0u;
+  return phys < 0 ? -1 : (((int64_t)h * a.max_pages + phys) << a.page_shift) + (p & (a.page_size - 1));
+}
+// Their keys; NaN where they have no page
+__device__ __forceinline__ void load_keys(const KeepLaunch& a, const Unit& u, int64_t at, int p, uint32_t (&key)[4]) {
+  const float nan = __builtin_nanf("");
+  float4 v = make_float4(nan, nan, nan, nan);
+  if (at >= 0 && p < u.kv) v = *reinterpret_cast<const float4*>(a.mass + at);
+  const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    key[e] = p + e >= u.kv ? kAbsent : p + e < u.sink || p + e >= u.end ? kAlways : mass_key(f[e]);
 }
 
-// The bin that holds the need-th largest key, and how many of the bin's keys are taken; c0, c1: the thread's two bins'
-// counts (bins 2 t, 2 t + 1).  need >= 1 and at most all of them.
-__device__ __forceinline__ void find_bin(int c0, int c1, int need, int* wave_tot, int* found, int& bin, int& rest) {
-  int all;
-  const int before = block_exclusive_scan<kThreads>(c0 + c1, wave_tot, all);
-  const int above1 = all - before - c0 - c1, above0 = above1 + c1;  // keys in higher bins
-  const int t = threadIdx.x;
-  if (above1 < need && need <= above1 + c1) {
-    found[0] = 2 * t + 1;
-    found[1] = need - above1;
+struct KeepLds {
+  uint32_t hist[kCopies * kCopyPitch];  // a list lies behind the first copy
+  int wave_tot[kWaves], found[4], listed;
+  __device__ __forceinline__ uint32_t* list() { return hist + kCopyPitch; }
+};
+static_assert(kListed <= (kCopies - 1) * kCopyPitch, "the list's room");
+// The threshold: key, and how many tokens of it are taken
+struct Taken {
+  uint32_t key;
+  int ties;
+};
+
+// COPIES 8: for counts of all keys; 1: of a list of few, whose lanes wait for each other for as many cycles as it has keys at most
+template <int COPIES>
+__device__ __forceinline__ void clear_bins(KeepLds& S) {
+  for (int x = threadIdx.x; x < COPIES * kCopyPitch / 4; x += kThreads) reinterpret_cast<uint4*>(S.hist)[x] = make_uint4(0, 0, 0, 0);
+  __syncthreads();
+}
+template <int COPIES>
+__device__ __forceinline__ void count_bin(KeepLds& S, uint32_t bin) {
+  atomicAdd(&S.hist[(threadIdx.x & (COPIES - 1)) * kCopyPitch + bin], 1u);
+}
+// Counts of the thread's two bins, 2 t and 2 t + 1, once all threads have counted
+template <int COPIES>
+__device__ __forceinline__ uint2 own_bins(const KeepLds& S) {
+  __syncthreads();
+  uint2 c = make_uint2(0, 0);
+#pragma unroll
+  for (int x = 0; x < COPIES; ++x) {
+    const uint2 y = *reinterpret_cast<const uint2*>(&S.hist[x * kCopyPitch + 2 * threadIdx.x]);
+    c.x += y.x;
+    c.y += y.y;
+  }
+  return c;
+}
+
+// The bin that holds the need-th largest key, how many of the bin's keys are taken, and how many it has; c: the counts of the
+// thread's two bins.  need >= 1 and at most all of them.  Calls of it have a barrier between them.
+__device__ __forceinline__ void find_bin(KeepLds& S, uint2 c, int need, int& bin, int& rest, int& size) {
+  const int c0 = (int)c.x, c1 = (int)c.y, t = threadIdx.x, w = t / kWave;
+  const int inc = wave_inclusive_scan(c0 + c1);
+  if (lane_id() == kWave - 1) S.wave_tot[w] = inc;
+  __syncthreads();
+  int above1 = -inc;  // keys in higher bins than the thread's
+#pragma unroll
+  for (int x = 0; x < kWaves; ++x) above1 += x >= w ? S.wave_tot[x] : 0;
+  const int above0 = above1 + c1;
+  if (above1 < need && need <= above0) {
+    S.found[0] = 2 * t + 1;
+    S.found[1] = need - above1;
+    S.found[2] = c1;
   }
   if (above0 < need && need <= above0 + c0) {
-    found[0] = 2 * t;
-    found[1] = need - above0;
+    S.found[0] = 2 * t;
+    S.found[1] = need - above0;
+    S.found[2] = c0;
   }
   __syncthreads();
-  bin = found[0];
-  rest = found[1];
-  __syncthreads();
+  bin = S.found[0];
+  rest = S.found[1];
+  size = S.found[2];
 }
 
-struct Taken {
-  uint32_t key;  // the threshold
-  int ties;      // of its key, the first so many are taken
-};
-// Whether the token at p is kept for certain, and whether it is of the threshold's key
-__device__ __forceinline__ void classify(const Unit& u, const Taken& tk, int p, uint32_t key, bool& gt, bool& tie) {
-  const bool choice = p >= u.sink && p < u.end;
-  gt = p < u.kv && (!choice || key > tk.key);
-  tie = choice && key == tk.key;
+// The threshold among keys that begin with `prefix` (11 bits): the need-th largest.  each(f) calls f for the thread's part of
+// them, or of keys that they are among.
+template <int COPIES, class Each>
+__device__ __forceinline__ Taken threshold(KeepLds& S, uint32_t prefix, int need, Each&& each) {
+  int bin, size;
+  clear_bins<COPIES>(S);
+  each([&](uint32_t k) { if (k >> 21 == prefix) count_bin<COPIES>(S, (k >> 10) & 2047u); });
+  find_bin(S, own_bins<COPIES>(S), need, bin, need, size);
+  const uint32_t both = prefix << 11 | (uint32_t)bin;
+  clear_bins<COPIES>(S);
+  each([&](uint32_t k) { if (k >> 10 == both) count_bin<COPIES>(S, k & 1023u); });
+  find_bin(S, own_bins<COPIES>(S), need, bin, need, size);
+  return {both << 10 | (uint32_t)bin, need};
 }
+
+// (key > the threshold: kept for certain, 1; of the threshold's key: 2^16)
+__device__ __forceinline__ uint32_t classify(const Taken& tk, uint32_t key) {
+  return (key > tk.key ? 1u : 0u) + (key == tk.key ? 1u << 16 : 0u);
+}
+constexpr Taken kNoneByMass = {kAlways - 1, 0};
 
 template <int ITS>
 __global__ __launch_bounds__(kThreads) void keep_kernel(const KeepLaunch a) {
-  __shared__ uint32_t hist[kBins * kCopies];
-  __shared__ int wave_tot[kWaves], found[2];
-  __shared__ int tot_gt[ITS * kWaves], tot_tie[ITS * kWaves];
+  __shared__ __align__(16) KeepLds S;
+  __shared__ uint32_t totals[ITS * kWaves];
   const int t = threadIdx.x, lane = lane_id(), w = t / kWave;
   const int h = blockIdx.x, s = blockIdx.y;
+  int64_t at[ITS];
+#pragma unroll
+  for (int it = 0; it < ITS; ++it) {
+    const int p = it * 4 * kThreads + 4 * t;
+    at[it] = p < a.b.max_kv ? find_keys(a, s, h, p) : -1;
+  }
   const Unit u = unit_of(a, s);
   if (t == 0 && h == 0) a.kept[s] = u.count;
   int32_t* const out = a.keep + ((int64_t)s * a.num_kv_heads + h) * a.budget;
@@ -100,228 +169,238 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(const KeepLaunch a) {
   }
   uint32_t key[ITS][4];
 #pragma unroll
-  for (int it = 0; it < ITS; ++it) {
-    const int p = it * 4 * kThreads + 4 * t;
-    key[it][0] = key[it][1] = key[it][2] = key[it][3] = 0u;
-    if (p < u.kv) load_keys(a, s, h, p, u.kv, key[it]);
-  }
-  int need = u.count - u.sink - (u.kv - u.end);
-  Taken tk = {0xffffffffu, 0};
+  for (int it = 0; it < ITS; ++it) load_keys(a, u, at[it], it * 4 * kThreads + 4 * t, key[it]);
+  Taken tk = kNoneByMass;
+  int need = chosen(u);
   if (need > 0) {
-    uint32_t prefix = 0;
-    for (int level = 0; level < 3; ++level) {
-      for (int x = t; x < kBins * kCopies; x += kThreads) hist[x] = 0;
-      __syncthreads();
-      const int shift = level == 0 ? 32 : level == 1 ? 21 : 10;
+    const auto each = [&](auto&& f) {
 #pragma unroll
       for (int it = 0; it < ITS; ++it)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int p = it * 4 * kThreads + 4 * t + e;
-          const bool in = p >= u.sink && p < u.end && (level == 0 || key[it][e] >> shift == prefix);
-          if (in) atomicAdd(&hist[bin_of(key[it][e], level) * kCopies + (lane & (kCopies - 1))], 1u);
-        }
-      __syncthreads();
-      int c0 = 0, c1 = 0;
-#pragma unroll
-      for (int x = 0; x < kCopies; ++x) {
-        c0 += (int)hist[2 * t * kCopies + x];
-        c1 += (int)hist[(2 * t + 1) * kCopies + x];
-      }
-      int bin, rest;
-      find_bin(c0, c1, need, wave_tot, found, bin, rest);
-      prefix = level == 0 ? (uint32_t)bin : (prefix << (level == 1 ? 11 : 10)) | (uint32_t)bin;
-      need = rest;
+        for (int e = 0; e < 4; ++e)
+          if (by_mass(key[it][e])) f(key[it][e]);
+    };
+    int bin, size;
+    if (t == 0) S.listed = 0;
+    clear_bins<kCopies>(S);
+    each([&](uint32_t k) { count_bin<kCopies>(S, k >> 21); });
+    find_bin(S, own_bins<kCopies>(S), need, bin, need, size);
+    const uint32_t prefix = (uint32_t)bin;
+    if (size > kListed) {
+      tk = threshold<kCopies>(S, prefix, need, each);
+    } else {
+      each([&](uint32_t k) {
+        if (k >> 21 != prefix) return;
+        const int at = atomicAdd(&S.listed, 1);
+        if (at < kListed) S.list()[at] = k;
+      });
+      tk = threshold<1>(S, prefix, need, [&](auto&& f) {
+        for (int x = t; x < size; x += kThreads) f(S.list()[x]);
+      });
     }
-    tk.key = prefix;
-    tk.ties = need;
   }
-  // places: counts of each (step, wave), then within the wave
-  int in_gt[ITS], in_tie[ITS];
+  // places: counts of each (step, wave), tokens that are taken for certain in the lower half of a word and ties in the
+  // upper, then within the wave
+  uint32_t inside[ITS];
 #pragma unroll
   for (int it = 0; it < ITS; ++it) {
-    int g = 0, e4 = 0;
+    uint32_t n = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      bool gt, tie;
-      classify(u, tk, it * 4 * kThreads + 4 * t + e, key[it][e], gt, tie);
-      g += gt;
-      e4 += tie;
-    }
-    in_gt[it] = wave_inclusive_scan(g);
-    in_tie[it] = wave_inclusive_scan(e4);
-    if (lane == kWave - 1) {
-      tot_gt[it * kWaves + w] = in_gt[it];
-      tot_tie[it * kWaves + w] = in_tie[it];
-    }
-    in_gt[it] -= g;
-    in_tie[it] -= e4;
+    for (int e = 0; e < 4; ++e) n += classify(tk, key[it][e]);
+    inside[it] = (uint32_t)wave_inclusive_scan((int)n);
+    if (lane == kWave - 1) totals[it * kWaves + w] = inside[it];
+    inside[it] -= n;
   }
   __syncthreads();
-  if (w == 0) {  // exclusive sums over the (step, wave)s, 64 at a time
-    int base_g = 0, base_t = 0;
-    for (int x = lane; x < (ITS * kWaves + kWave - 1) / kWave * kWave; x += kWave) {
-      const int g = x < ITS * kWaves ? tot_gt[x] : 0, e4 = x < ITS * kWaves ? tot_tie[x] : 0;
-      const int ig = wave_inclusive_scan(g), ie = wave_inclusive_scan(e4);
-      if (x < ITS * kWaves) {
-        tot_gt[x] = base_g + ig - g;
-        tot_tie[x] = base_t + ie - e4;
-      }
-      base_g += __builtin_amdgcn_readlane(ig, kWave - 1);
-      base_t += __builtin_amdgcn_readlane(ie, kWave - 1);
-    }
+  // every wave adds the totals up for itself, 64 at a time
+  constexpr int kSums = (ITS * kWaves + kWave - 1) / kWave;
+  uint32_t before[kSums], base = 0;
+#pragma unroll
+  for (int x = 0; x < kSums; ++x) {
+    const uint32_t n = x * kWave + lane < ITS * kWaves ? totals[x * kWave + lane] : 0u;
+    const uint32_t sum = (uint32_t)wave_inclusive_scan((int)n);
+    before[x] = base + sum - n;
+    base += (uint32_t)__builtin_amdgcn_readlane((int)sum, kWave - 1);
   }
-  __syncthreads();
+  const int ws = __builtin_amdgcn_readfirstlane(w);
 #pragma unroll
   for (int it = 0; it < ITS; ++it) {
-    int g = tot_gt[it * kWaves + w] + in_gt[it], e4 = tot_tie[it * kWaves + w] + in_tie[it];
+    uint32_t n = (uint32_t)__builtin_amdgcn_readlane((int)before[it * kWaves / kWave], it * kWaves % kWave + ws) + inside[it];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int p = it * 4 * kThreads + 4 * t + e;
-      bool gt, tie;
-      classify(u, tk, p, key[it][e], gt, tie);
-      const int at = g + min(e4, tk.ties);
-      if ((gt || (tie && e4 < tk.ties)) && (uint32_t)at < (uint32_t)u.count) out[at] = p;
-      g += gt;
-      e4 += tie;
+      const uint32_t kind = classify(tk, key[it][e]);
+      const int ties = (int)(n >> 16), at = (int)(n & 0xffffu) + min(ties, tk.ties);
+      if ((kind == 1 || (kind > 1 && ties < tk.ties)) && (uint32_t)at < (uint32_t)u.count) out[at] = it * 4 * kThreads + 4 * t + e;
+      n += kind;
     }
   }
 }
 
 // -------------------------------------------------------------------------------------
-// Several chunks.  Device memory of a unit (sequence, KV head): counts [3][chunks][kBins], above [chunks] (tokens of a
-// chunk above the threshold as far as it is known, or always kept), state [4] (bins and remaining needs of the levels
-// that are done).
-__device__ __forceinline__ uint32_t* unit_words(const KeepLaunch& a, int s, int h) {
-  return a.counts + ((int64_t)s * a.num_kv_heads + h) * keep_words(a);
+// Several chunks.  Device memory of a unit (sequence, KV head): counts [chunks][kBins] of the first bits; above [chunks], a
+// chunk's keys in higher bins than the threshold's; state [4]: the length of the list, the threshold's bin, the keys of
+// it that are taken; list [chunks * chunk] (key, chunk), in any order.
+struct UnitWords {
+  uint32_t* counts;
+  uint32_t* above;
+  uint32_t* state;
+  uint2* list;
+};
+__device__ __forceinline__ UnitWords unit_words(const KeepLaunch& a, int s, int h) {
+  UnitWords w;
+  w.counts = a.counts + ((int64_t)s * a.num_kv_heads + h) * keep_words(a);
+  w.above = w.counts + (int64_t)a.chunks * kBins;
+  w.state = w.above + kMaxChunks;
+  w.list = reinterpret_cast<uint2*>(w.state + 4);
+  return w;
 }
 
-// The thread's two bins of all chunks that have tokens
-__device__ __forceinline__ void sum_bins(const uint32_t* counts, int chunks, int& c0, int& c1) {
-  c0 = c1 = 0;
-#pragma unroll 16
-  for (int c = 0; c < chunks; ++c) {
-    const uint2 x = *reinterpret_cast<const uint2*>(counts + (int64_t)c * kBins + 2 * threadIdx.x);
-    c0 += (int)x.x;
-    c1 += (int)x.y;
-  }
+struct Chunk {
+  int c, h, s, begin, end, chunks;
+};
+__device__ __forceinline__ Chunk chunk_of(const KeepLaunch& a, const Unit& u) {
+  Chunk r;
+  r.c = blockIdx.x;
+  r.h = blockIdx.y;
+  r.s = blockIdx.z;
+  r.begin = (int)min((int64_t)r.c * a.chunk, (int64_t)u.kv);
+  r.end = (int)min((int64_t)r.begin + a.chunk, (int64_t)u.kv);
+  r.chunks = (u.kv + a.chunk - 1) / a.chunk;
+  return r;
 }
 
-// LEVEL 0..2: the counts of a level's bits, of the chunk's keys that begin with the bins found before
-template <int LEVEL>
 __global__ __launch_bounds__(kThreads) void keep_count_kernel(const KeepLaunch a) {
-  __shared__ uint32_t hist[kBins * kCopies];
-  __shared__ int wave_tot[kWaves], found[2];
+  __shared__ __align__(16) KeepLds S;
+  const int t = threadIdx.x;
+  const Unit u = unit_of(a, blockIdx.z);
+  const Chunk k = chunk_of(a, u);
+  if (chosen(u) <= 0 || k.begin >= k.end) return;
+  const UnitWords m = unit_words(a, k.s, k.h);
+  if (k.c == 0 && t == 0) m.state[0] = 0;
+  clear_bins<kCopies>(S);
+#pragma unroll 2
+  for (int p0 = k.begin + 4 * t; p0 < k.end; p0 += 4 * kThreads) {
+    uint32_t key[4];
+    load_keys(a, u, find_keys(a, k.s, k.h, p0), p0, key);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (by_mass(key[e])) count_bin<kCopies>(S, key[e] >> 21);
+  }
+  *reinterpret_cast<uint2*>(m.counts + (int64_t)k.c * kBins + 2 * t) = own_bins<kCopies>(S);
+}
+
+__global__ __launch_bounds__(kThreads) void keep_list_kernel(const KeepLaunch a) {
+  __shared__ __align__(16) KeepLds S;
   const int t = threadIdx.x, lane = lane_id();
-  const int c = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
-  const Unit u = unit_of(a, s);
-  const int need = u.count - u.sink - (u.kv - u.end);
-  if (need <= 0 || (int64_t)c * a.chunk >= u.kv) return;
-  const int begin = c * a.chunk, end = (int)min((int64_t)u.kv, (int64_t)begin + a.chunk);
-  const int chunks = (u.kv + a.chunk - 1) / a.chunk;
-  uint32_t* const words = unit_words(a, s, h);
-  uint32_t* const above = words + 3 * (int64_t)a.chunks * kBins;
-  uint32_t* const state = above + a.chunks;
-  uint32_t prefix = 0;
-  if constexpr (LEVEL > 0) {
-    // the bin of the level before, by every workgroup; this chunk's keys above it
-    const uint32_t* before = words + (LEVEL - 1) * (int64_t)a.chunks * kBins;
-    int c0, c1, bin, rest;
-    sum_bins(before, chunks, c0, c1);
-    find_bin(c0, c1, LEVEL == 1 ? need : (int)state[1], wave_tot, found, bin, rest);
-    prefix = LEVEL == 1 ? (uint32_t)bin : state[0] << 11 | (uint32_t)bin;
-    const uint2 own = *reinterpret_cast<const uint2*>(before + (int64_t)c * kBins + 2 * t);
-    const int more = block_sum<kThreads>((2 * t > bin ? (int)own.x : 0) + (2 * t + 1 > bin ? (int)own.y : 0), wave_tot);
-    if (t == 0) above[c] = (LEVEL == 1 ? 0u : above[c]) + (uint32_t)more;
-    // (LEVEL 2 reads state[0..1] and writes state[2..3]: no workgroup changes what another reads)
-    if (c == 0 && t == 0) {
-      state[2 * (LEVEL - 1)] = prefix;
-      state[2 * (LEVEL - 1) + 1] = (uint32_t)rest;
+  const Unit u = unit_of(a, blockIdx.z);
+  const Chunk k = chunk_of(a, u);
+  const int need = chosen(u);
+  if (need <= 0 || k.begin >= k.end) return;
+  const UnitWords m = unit_words(a, k.s, k.h);
+  // the chunk's first keys are on their way while the counts are added up
+  const int p1 = k.begin + 4 * t;
+  uint32_t key[4] = {kAbsent, kAbsent, kAbsent, kAbsent};
+  if (p1 < k.end) load_keys(a, u, find_keys(a, k.s, k.h, p1), p1, key);
+  const uint2 own = *reinterpret_cast<const uint2*>(m.counts + (int64_t)k.c * kBins + 2 * t);
+  uint2 sum = make_uint2(0, 0);
+#pragma unroll 16
+  for (int c = 0; c < k.chunks; ++c) {
+    const uint2 x = *reinterpret_cast<const uint2*>(m.counts + (int64_t)c * kBins + 2 * t);
+    sum.x += x.x;
+    sum.y += x.y;
+  }
+  int bin, rest, size;
+  find_bin(S, sum, need, bin, rest, size);
+  __syncthreads();
+  const int above = block_sum<kThreads>((2 * t > bin ? (int)own.x : 0) + (2 * t + 1 > bin ? (int)own.y : 0), S.wave_tot);
+  if (t == 0) {
+    m.above[k.c] = (uint32_t)above;
+    if (k.c == 0) {
+      m.state[1] = (uint32_t)bin;
+      m.state[2] = (uint32_t)rest;
     }
   }
-  for (int x = t; x < kBins * kCopies; x += kThreads) hist[x] = 0;
+  if (2 * t == (bin & ~1)) S.listed = (int)atomicAdd(&m.state[0], bin & 1 ? own.y : own.x);  // this chunk's part of the list
   __syncthreads();
-  for (int p0 = begin + 4 * t; p0 < end; p0 += 4 * kThreads) {
-    uint32_t key[4];
-    load_keys(a, s, h, p0, u.kv, key);
+  for (int p0 = p1; p0 - 4 * t < k.end; p0 += 4 * kThreads) {
+    if (p0 != p1 && p0 < k.end) load_keys(a, u, find_keys(a, k.s, k.h, p0), p0, key);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int p = p0 + e;
-      const bool in = p >= u.sink && p < u.end && (LEVEL == 0 || key[e] >> (LEVEL == 1 ? 21 : 10) == prefix);
-      if (in) atomicAdd(&hist[bin_of(key[e], LEVEL) * kCopies + (lane & (kCopies - 1))], 1u);
+      const bool in = p0 < k.end && by_mass(key[e]) && key[e] >> 21 == (uint32_t)bin;
+      const uint64_t all = __ballot(in);
+      if (!all) continue;
+      int base = 0;
+      if (lane == 0) base = atomicAdd(&S.listed, (int)__popcll(all));
+      base = __builtin_amdgcn_readfirstlane(base) + lanes_below(all);
+      if (in && (uint32_t)base < (uint32_t)(a.chunks * (int64_t)a.chunk)) m.list[base] = make_uint2(key[e], (uint32_t)k.c);
     }
   }
-  __syncthreads();
-  uint2 sum = make_uint2(0, 0);
-#pragma unroll
-  for (int x = 0; x < kCopies; ++x) {
-    sum.x += hist[2 * t * kCopies + x];
-    sum.y += hist[(2 * t + 1) * kCopies + x];
-  }
-  *reinterpret_cast<uint2*>(words + (LEVEL * (int64_t)a.chunks + c) * kBins + 2 * t) = sum;
 }
 
 __global__ __launch_bounds__(kThreads) void keep_write_kernel(const KeepLaunch a) {
-  __shared__ int wave_tot[kWaves], found[2];
+  __shared__ __align__(16) KeepLds S;
   const int t = threadIdx.x;
-  const int c = blockIdx.x, h = blockIdx.y, s = blockIdx.z;
-  const Unit u = unit_of(a, s);
-  if (c == 0 && h == 0 && t == 0) a.kept[s] = u.count;
-  if ((int64_t)c * a.chunk >= u.kv) return;
-  const int begin = c * a.chunk, end = (int)min((int64_t)u.kv, (int64_t)begin + a.chunk);
-  const int chunks = (u.kv + a.chunk - 1) / a.chunk;
-  int32_t* const out = a.keep + ((int64_t)s * a.num_kv_heads + h) * a.budget;
-  const int need = u.count - u.sink - (u.kv - u.end);
+  const Unit u = unit_of(a, blockIdx.z);
+  const Chunk k = chunk_of(a, u);
+  if (k.c == 0 && k.h == 0 && t == 0) a.kept[k.s] = u.count;
+  if (k.begin >= k.end) return;
+  int32_t* const out = a.keep + ((int64_t)k.s * a.num_kv_heads + k.h) * a.budget;
   // tokens before the chunk: always kept ones, ones above the threshold, ones of its key
-  int gt = min(begin, u.sink) + max(begin - u.end, 0), tie = 0;
-  Taken tk = {0xffffffffu, 0};
-  if (need > 0) {
-    const uint32_t* words = unit_words(a, s, h);
-    const uint32_t* above = words + 3 * (int64_t)a.chunks * kBins;
-    const uint32_t* state = above + a.chunks;
-    const uint32_t* last = words + 2 * (int64_t)a.chunks * kBins;
-    int c0, c1, bin, rest;
-    sum_bins(last, chunks, c0, c1);
-    find_bin(c0, c1, (int)state[3], wave_tot, found, bin, rest);
-    tk.key = state[2] << 10 | (uint32_t)bin;
-    tk.ties = rest;
-    int more = 0, same = 0;
-#pragma unroll 16
-    for (int x = 0; x < c; ++x) {
-      const uint2 own = *reinterpret_cast<const uint2*>(last + (int64_t)x * kBins + 2 * t);
-      more += (2 * t > bin ? (int)own.x : 0) + (2 * t + 1 > bin ? (int)own.y : 0);
-      same += 2 * t == bin ? (int)own.x : 2 * t + 1 == bin ? (int)own.y : 0;
-      if (t == 0) more += (int)above[x];
+  int gt = min(k.begin, u.sink) + max(k.begin - u.end, 0), tie = 0;
+  Taken tk = kNoneByMass;
+  const int p1 = k.begin + 4 * t;
+  uint32_t key[4] = {kAbsent, kAbsent, kAbsent, kAbsent};
+  if (p1 < k.end) load_keys(a, u, find_keys(a, k.s, k.h, p1), p1, key);
+  if (chosen(u) > 0) {
+    const UnitWords m = unit_words(a, k.s, k.h);
+    const int n = (int)min((int64_t)m.state[0], a.chunks * (int64_t)a.chunk);
+    const int need = (int)m.state[2];
+    const int above = t < k.c ? (int)m.above[t] : 0;  // (at most 64 chunks)
+    const uint32_t prefix = m.state[1];
+    int g = above, e = 0;
+    if (n <= kListed) {
+      for (int x = t; x < n; x += kThreads) S.list()[x] = m.list[x].x;
+      tk = threshold<1>(S, prefix, need, [&](auto&& f) {
+        for (int x = t; x < n; x += kThreads) f(S.list()[x]);
+      });
+    } else {
+      tk = threshold<kCopies>(S, prefix, need, [&](auto&& f) {
+#pragma unroll 4
+        for (int x = t; x < n; x += kThreads) f(m.list[x].x);
+      });
     }
-    gt += block_sum<kThreads>(more, wave_tot);
-    tie += block_sum<kThreads>(same, wave_tot);
+#pragma unroll 4
+    for (int x = t; x < n; x += kThreads) {
+      const uint2 y = m.list[x];
+      const bool before = (int)y.y < k.c;
+      g += before && y.x > tk.key;
+      e += before && y.x == tk.key;
+    }
+    __syncthreads();
+    gt += block_sum<kThreads>(g, S.wave_tot);
+    tie += block_sum<kThreads>(e, S.wave_tot);
   }
-  for (int p0 = begin; p0 < end; p0 += 4 * kThreads) {
+  for (int p0 = k.begin; p0 < k.end; p0 += 4 * kThreads) {
     const int p4 = p0 + 4 * t;
-    uint32_t key[4] = {0u, 0u, 0u, 0u};
-    if (p4 < end) load_keys(a, s, h, p4, u.kv, key);
-    bool g[4], e[4];
-    int ng = 0, ne = 0;
+    if (p0 != k.begin && p4 < k.end) load_keys(a, u, find_keys(a, k.s, k.h, p4), p4, key);
+    uint32_t kind[4], n = 0;  // (at most 4096 of each in a step)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      classify(u, tk, p4 + i, key[i], g[i], e[i]);
-      g[i] = g[i] && p4 + i < end;
-      e[i] = e[i] && p4 + i < end;
-      ng += g[i];
-      ne += e[i];
+      kind[i] = p4 < k.end ? classify(tk, key[i]) : 0;
+      n += kind[i];
     }
-    int all_g, all_e;
-    int at_g = gt + block_exclusive_scan<kThreads>(ng, wave_tot, all_g);
-    int at_e = tie + block_exclusive_scan<kThreads>(ne, wave_tot, all_e);
+    int all;
+    const int before = block_exclusive_scan<kThreads>((int)n, S.wave_tot, all);
+    int at_g = gt + (before & 0xffff), at_e = tie + (before >> 16);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int at = at_g + min(at_e, tk.ties);
-      if ((g[i] || (e[i] && at_e < tk.ties)) && (uint32_t)at < (uint32_t)u.count) out[at] = p4 + i;
-      at_g += g[i];
-      at_e += e[i];
+      if ((kind[i] == 1 || (kind[i] > 1 && at_e < tk.ties)) && (uint32_t)at < (uint32_t)u.count) out[at] = p4 + i;
+      at_g += (int)(kind[i] & 1);
+      at_e += (int)(kind[i] >> 16);
     }
-    gt += all_g;
-    tie += all_e;
+    gt += all & 0xffff;
+    tie += all >> 16;
   }
 }
 
@@ -422,8 +501,7 @@ hipError_t launch_keep(const KeepLaunch& a, hipStream_t stream) {
     return launch_one(f, dim3(a.num_kv_heads, a.b.n_seqs), kThreads, stream, a);
   }
   const dim3 grid(a.chunks, a.num_kv_heads, a.b.n_seqs);
-  for (const void* f : {(const void*)keep_count_kernel<0>, (const void*)keep_count_kernel<1>, (const void*)keep_count_kernel<2>,
-                        (const void*)keep_write_kernel}) {
+  for (const void* f : {(const void*)keep_count_kernel, (const void*)keep_list_kernel, (const void*)keep_write_kernel}) {
     const hipError_t e = launch_one(f, grid, kThreads, stream, a);
     if (e != hipSuccess) return e;
   }
