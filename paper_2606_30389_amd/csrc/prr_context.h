@@ -105,7 +105,6 @@ struct MassLaunch {
   bool bf16, e4m3;
   ShapeArgs sh;
   int shape;
-  float k2[5];  // sh.k in the units of the exponent
 };
 
 struct KeepLaunch {

@@ -122,6 +122,27 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(const MassLaunch a) {
       if (prefix <= g0) i0 = max(i0, g0 - first);
       if (a.sh.window) i1 = (int)max(min((int64_t)i1, (int64_t)g1 + a.sh.window - 1 - first), (int64_t)0);
     }
+    if (a.sh.first && !a.pages) {  // (documents: the first and the last token that see a key of the workgroup's)
+      const int g0 = kg * 64 * KB, g1 = (int)min((int64_t)g0 + 64 * KB, keys);
+      int lo = 0x7fffffff, hi = 0;
+      for (int i = i0 + t; i < i1; i += 256) {
+        const Span sp = span_at(a.sh.window, a.sh.first[sq.q0 + i], prefix, first + i, sq.kv);
+        if (sp.lo < min(sp.hi, g1) && sp.hi > g0) {
+          lo = min(lo, i);
+          hi = i + 1;
+        }
+      }
+      lo = (int)wave_umin((uint32_t)lo);
+      hi = (int)wave_umax((uint32_t)hi);
+      if (lane == 0) {
+        l_lo[0][w] = lo;
+        l_hi[0][w] = hi;
+      }
+      __syncthreads();
+      i0 = min(min(l_lo[0][0], l_lo[0][1]), min(l_lo[0][2], l_lo[0][3]));
+      i1 = max(max(l_hi[0][0], l_hi[0][1]), max(l_hi[0][2], l_hi[0][3]));
+      __syncthreads();
+    }
     const int rows = max(i1 - i0, 0) * G, tiles = (rows + kRows - 1) / kRows;
     const int per = (tiles + a.nsplit - 1) / a.nsplit;
     const int t0 = min(part * per, tiles), t1 = min(t0 + per, tiles);
@@ -139,30 +160,50 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(const MassLaunch a) {
 
     // Thread t brings 16 bytes of rows t/16 + 16 x; the place of row r's 16 bytes c is c ^ (r % 16), so that a read of the
     // same bytes of 16 rows meets every bank once.  Threads 0..63 bring what is known of row t.  Nothing of it is looked at
-    // before the products of the tile before are done.
+    // before the products of the tile before are done.  A row lies at an offset from the tile's first token that is the same
+    // in every tile where the group size divides 64.
     u32x4_t qr[4];
+    uint32_t offset[4], info = 0;  // bytes; rows of m and l
     float r_m = 0.0f, r_l = 0.0f, r_slope = 0.0f;
-    int r_first = 0, r_pos = 0;
+    int r_first = 0, r_tok = 0, r_pos = 0;
     bool r_live = false;
-    const auto load = [&](int tile) {
+    const bool aligned = (G & (G - 1)) == 0;
+    const int heads = a.c.num_kv_heads * G;
+    const auto tile_token = [&](int tile) { return mass_over_group(tile * kRows, a.magic); };
+    const auto load = [&](int tile, bool find) {
+      const int r0 = tile * kRows, tok0 = tile_token(tile), h0 = r0 - tok0 * G;
+      if (find || !aligned || r0 + kRows > rows) {
+        const auto at = [&](int local, int& tok, int& head) {
+          const int r = h0 + min(local, rows - 1 - r0);
+          tok = mass_over_group(r, a.magic);
+          head = r - tok * G;
+          return (uint32_t)(tok * heads + head);
+        };
+        int tok, head;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int r = min(tile * kRows + (t >> 4) + 16 * x, rows - 1);
-        const int tok = mass_over_group(r, a.magic), head = r - tok * G;
-        const int64_t at = ((int64_t)(sq.q0 + i0 + tok) * a.c.num_kv_heads + h) * G + head;
-        qr[x] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q) + at * kHeadDim + 8 * (t & 15));
+        for (int x = 0; x < 4; ++x) offset[x] = at((t >> 4) + 16 * x, tok, head) * (2 * kHeadDim) + 16 * (t & 15);
+        if (t < kRows) {
+          info = at(t, r_tok, head);
+          if constexpr (SHAPE & kShapeSlopes) r_slope = a.sh.slopes[h * G + head] * kRawPerLogit;
+        }
       }
+      const int64_t row = ((int64_t)(sq.q0 + i0 + tok0) * a.c.num_kv_heads + h) * G;
+      const char* const q = static_cast<const char*>(a.q) + row * (2 * kHeadDim);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) qr[x] = *reinterpret_cast<const u32x4_t*>(q + offset[x]);
       if (t < kRows) {
-        const int r = min(tile * kRows + t, rows - 1);
-        const int tok = mass_over_group(r, a.magic), head = r - tok * G;
-        const int64_t at = ((int64_t)(sq.q0 + i0 + tok) * a.c.num_kv_heads + h) * G + head;
-        r_m = a.m[at];
-        r_l = a.l[at];
-        r_first = a.sh.first ? a.sh.first[sq.q0 + i0 + tok] : 0;
-        r_pos = first + i0 + tok;
-        r_live = tile * kRows + t < rows;  // (rows behind the last see nothing)
-        if constexpr (SHAPE & kShapeSlopes) r_slope = a.sh.slopes[h * G + head] * kRawPerLogit;
+        r_m = (a.m + row)[info];
+        r_l = (a.l + row)[info];
+        r_first = a.sh.first ? (a.sh.first + sq.q0 + i0 + tok0)[r_tok] : 0;
+        r_pos = first + i0 + tok0 + r_tok;
+        r_live = r0 + t < rows;  // (rows behind the last see nothing)
       }
+    };
+    // Whether the wave's keys are seen by every row of a tile, as far as that is known without looking at the rows
+    const auto known_whole = [&](int tile) {
+      if (!run || a.sh.first || (tile + 1) * kRows > rows || wk1 == 0) return false;
+      const int p0 = first + i0 + tile_token(tile), p1 = first + i0 + mass_over_group(tile * kRows + kRows - 1, a.magic);
+      return max(p0 + 1, prefix) >= wk1 && (!a.sh.window || p1 - a.sh.window + 1 <= wk0);
     };
     const auto store = [&](int buf) {
 #pragma unroll
@@ -224,29 +265,23 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(const MassLaunch a) {
           for (int i = 0; i < 4; ++i) d[b][i] = fmaf(-slope, fabsf(ahead + (float)i), d[b][i]);
         }
       }
-      // (the change to powers of two is in k2 where nothing comes between)
-      const auto weight = [&](float x) { return exp2_hw(fmaf(x, kSoftmaxScale2, -ref)); };
       if constexpr (SHAPE == kShapeCap) {
         if (small) {
 #pragma unroll
           for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) d[b][i] = exp2_hw(fmaf(d[b][i], cap_ratio(d[b][i], a.k2, kSoftmaxScale2), -ref));
+            for (int i = 0; i < 4; ++i) d[b][i] = exp2_hw(cap_exponent(d[b][i], ref, kSoftmaxScale2, true, a.sh));
         } else {
 #pragma unroll
           for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float near = fmaf(d[b][i], cap_ratio(d[b][i], a.k2, kSoftmaxScale2), -ref);
-              const float far = fmaf(cap_large(d[b][i], a.sh), kSoftmaxScale2, -ref);
-              d[b][i] = exp2_hw(fabsf(d[b][i]) < a.sh.small ? near : far);
-            }
+            for (int i = 0; i < 4; ++i) d[b][i] = exp2_hw(cap_exponent(d[b][i], ref, kSoftmaxScale2, false, a.sh));
         }
       } else {
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) d[b][i] = weight(d[b][i]);
+          for (int i = 0; i < 4; ++i) d[b][i] = exp2_hw(fmaf(d[b][i], kSoftmaxScale2, -ref));
       }
       if constexpr (masked.value) {
         const int lo = l_lo[buf][16 * u + n], hi = l_hi[buf][16 * u + n];
@@ -261,32 +296,32 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(const MassLaunch a) {
       for (int b = 0; b < KB; ++b) sum[b] += d[b];
     };
     // The tile in the buffer: a lane looks at a row's keys
-    const auto tile_products = [&](int buf) {
+    const auto tile_products = [&](int tile, int buf) {
+      if (known_whole(tile)) {
+#pragma unroll
+        for (int u = 0; u < kRows / 16; ++u) products(buf, u, std::false_type{});
+        return;
+      }
       const int lo = l_lo[buf][lane], hi = l_hi[buf][lane];
       const uint64_t some = __ballot(lo < wk1 && hi > wk0 && lo < hi);
       const uint64_t whole = run ? __ballot(lo <= wk0 && hi >= wk1) : 0;
-      if (whole == ~0ull) {
-#pragma unroll
-        for (int u = 0; u < kRows / 16; ++u) products(buf, u, std::false_type{});
-      } else {
-        for (int u = 0; u < kRows / 16; ++u) {
-          if (((whole >> (16 * u)) & 0xffff) == 0xffff) {
-            products(buf, u, std::false_type{});
-          } else if ((some >> (16 * u)) & 0xffff) {
-            products(buf, u, std::true_type{});
-          }
+      for (int u = 0; u < kRows / 16; ++u) {
+        if (((whole >> (16 * u)) & 0xffff) == 0xffff) {
+          products(buf, u, std::false_type{});
+        } else if ((some >> (16 * u)) & 0xffff) {
+          products(buf, u, std::true_type{});
         }
       }
     };
 
     if (t0 < t1) {
-      load(t0);
+      load(t0, true);
       store(0);
       __syncthreads();
       for (int tile = t0; tile < t1; ++tile) {
         const int buf = (tile - t0) & 1;
-        if (tile + 1 < t1) load(tile + 1);
-        tile_products(buf);
+        if (tile + 1 < t1) load(tile + 1, false);
+        tile_products(tile, buf);
         if (tile + 1 < t1) store(buf ^ 1);
         if (flushes && ((tile - t0) & (kFlush - 1)) == kFlush - 1) {
 #pragma unroll

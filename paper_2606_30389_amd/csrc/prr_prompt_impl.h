@@ -293,7 +293,10 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
   };
   // Vector phase: the softmax of this tile.
   const auto vector = [&](int tile, auto masked) {
-    if constexpr (SHAPE & kShapeCap) {
+    // Where nothing comes between the cap and the exponent, the cap's product is the exponent's; the cap does not change
+    // the order of logits, so the largest is known before.
+    constexpr bool kFold = (SHAPE & kShapeCap) && !(SHAPE & kShapeSlopes) && !masked.value;
+    if constexpr ((SHAPE & kShapeCap) && !kFold) {
       float most = 0.0f;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -337,6 +340,16 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[b][i]);
+    [[maybe_unused]] bool near = false;
+    if constexpr (kFold) {
+      float least = sc[0][0];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) least = fminf(least, sc[b][i]);
+      near = __all(fmaxf(fabsf(top), fabsf(least)) < a.sh.small);
+      top = cap_any(top, a.sh);
+    }
     mx = fmaxf(mx, max_halves(top));
     const float scaled = mx * kSoftmaxScale2;
     const bool grown = scaled > ref + (kTop<BF16> + kSlack<BF16>);
@@ -348,13 +361,24 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
 #pragma unroll
       for (int cb = 0; cb < 4; ++cb) acc[cb] *= alpha;
     }
+    const auto weights = [&](auto&& exponent) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[b][i] = exp2_hw(fmaf(sc[b][i], kSoftmaxScale2, -ref));
-        l += sc[b][i];
+        for (int i = 0; i < 16; ++i) {
+          sc[b][i] = exp2_hw(exponent(sc[b][i]));
+          l += sc[b][i];
+        }
+    };
+    if constexpr (kFold) {
+      if (near) {
+        weights([&](float x) { return cap_exponent(x, ref, kSoftmaxScale2, true, a.sh); });
+      } else {
+        weights([&](float x) { return cap_exponent(x, ref, kSoftmaxScale2, false, a.sh); });
       }
+    } else {
+      weights([&](float x) { return fmaf(x, kSoftmaxScale2, -ref); });
+    }
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const int b = x >> 1, i = 8 * (x & 1);

@@ -13,7 +13,7 @@ struct ShapeArgs {
   const int32_t* first;
   int window;
   float cap, inv, small;  // the cap in the units of q.k, 1 / cap, the logits below which cap_small holds
-  float k[5];             // cap_small's coefficients
+  float k[5], k2[5];      // cap_small's coefficients, and in the units of the exponent
 };
 
 // Keys [lo, hi) of a sequence of kv tokens that the token at position pos (row `row` of the packed tensors) sees; lo = hi:
@@ -66,6 +66,14 @@ __device__ __forceinline__ float cap_large(float s, const ShapeArgs& a) {
 }
 __device__ __forceinline__ float cap_any(float s, const ShapeArgs& a) {
   return fabsf(s) < a.small ? cap_small(s, a) : cap_large(s, a);
+}
+
+// Exponents of weights relative to ref: log2(e) z / sqrt(128) - ref of capped logits, with the change of units in k2, so that
+// the product with s is the exponent's.  near: every logit of the caller's is below a.small.
+__device__ __forceinline__ float cap_exponent(float s, float ref, float scale2, bool near, const ShapeArgs& a) {
+  const float x = fmaf(s, cap_ratio(s, a.k2, scale2), -ref);
+  if (near) return x;
+  return fabsf(s) < a.small ? x : fmaf(cap_large(s, a), scale2, -ref);
 }
 
 #endif
