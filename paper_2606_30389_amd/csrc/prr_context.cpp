@@ -258,6 +258,7 @@ prr_status plan(const prr_dims* d, const prr_batch* b, int32_t kind, int32_t bud
   a.b = batch_args(b);
   cache_shape(d, a.c);
   a.budget = budget;
+  a.stage_rows = std::min(budget, b->max_kv);
   a.e4m3 = kind == PRR_KV_E4M3;
   return PRR_OK;
 }
@@ -578,10 +579,8 @@ prr_status prr_cache_compact(const prr_dims* dims, const prr_batch* batch, const
     PRR_TRY(prr::api_check_ptr(dst_table, "dst_table", 4));
     if (dst_table == batch->page_table)
       return api_fail(PRR_ERR_INVALID_ARG, "dst_table is the batch's page_table: NULL means in place");
-    const int64_t rows = std::min(budget, batch->max_kv);
-    if (dst_stride < 1 || (int64_t)dst_stride * dims->page_size < rows)
-      return api_fail(PRR_ERR_INVALID_ARG, "dst_stride %d: %lld tokens need more pages of %d", dst_stride, (long long)rows,
-                      dims->page_size);
+    if (dst_stride < 1 || (int64_t)dst_stride * dims->page_size < a.stage_rows)
+      return api_fail(PRR_ERR_INVALID_ARG, "dst_stride %d: %d tokens need more pages of %d", dst_stride, a.stage_rows, dims->page_size);
   } else {
     PRR_TRY(check_ws(workspace, ws_bytes, prr::compact_stage_bytes(a)));
   }

@@ -127,6 +127,7 @@ struct CompactLaunch {
   char* stage;               // rows on their way, in place
   BatchArgs b;
   int budget, dst_stride;
+  int stage_rows;  // of a sequence and KV head: no more can move
   int phase;  // 0: to other pages, 1: to the stage, 2: from the stage
   bool e4m3;
 };

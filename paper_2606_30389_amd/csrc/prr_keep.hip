@@ -423,7 +423,7 @@ __global__ __launch_bounds__(256) void compact_kernel(const CompactLaunch a) {
   const int kv = min(max(a.b.kv_len[s], 0), a.b.max_kv);
   const int count = min(max(a.kept[s], 0), min(a.budget, kv));
   const int64_t unit = (int64_t)s * a.c.num_kv_heads + h, units = (int64_t)a.b.n_seqs * a.c.num_kv_heads;
-  const int64_t stage_rows = units * a.budget;
+  const int64_t stage_row = unit * a.stage_rows, stage_rows = units * a.stage_rows;
   char* const stage_k = a.stage;
   char* const stage_v = stage_k + stage_rows * kRowBytes;
   float* const stage_mass = reinterpret_cast<float*>(stage_v + stage_rows * kRowBytes);
@@ -444,8 +444,8 @@ __global__ __launch_bounds__(256) void compact_kernel(const CompactLaunch a) {
         d = a.dst_table ? row_of(a.dst_table, a.dst_stride, (int)i) : row_of(a.b.page_table, a.b.table_stride, (int)i);
         if (f < 0 || f == d) d = -1;
         if (d < 0) f = -1;
-        if (a.phase == 1 && d >= 0) d = unit * a.budget + i;
-        if (a.phase == 2 && f >= 0) f = unit * a.budget + i;
+        if (a.phase == 1 && d >= 0) d = stage_row + i;
+        if (a.phase == 2 && f >= 0) f = stage_row + i;
       }
       from[t] = f;
       to[t] = d;
@@ -509,7 +509,7 @@ hipError_t launch_keep(const KeepLaunch& a, hipStream_t stream) {
 }
 
 size_t compact_stage_bytes(const CompactLaunch& a) {
-  const size_t rows = (size_t)a.b.n_seqs * a.c.num_kv_heads * a.budget;
+  const size_t rows = (size_t)a.b.n_seqs * a.c.num_kv_heads * a.stage_rows;
   const size_t bytes = rows * (2 * (a.e4m3 ? 128 : 256) + 4 + (a.e4m3 ? 2 : 0));
   return (bytes + 255) / 256 * 256;
 }
@@ -517,7 +517,7 @@ size_t compact_stage_bytes(const CompactLaunch& a) {
 hipError_t launch_compact(const CompactLaunch& a, hipStream_t stream) {
   const void* f = a.e4m3 ? (const void*)compact_kernel<true> : (const void*)compact_kernel<false>;
   const int64_t units = (int64_t)a.b.n_seqs * a.c.num_kv_heads;
-  const int64_t rows = min(a.budget, a.b.max_kv);
+  const int64_t rows = a.stage_rows;
   const int64_t blocks = max(min((rows + kMoveRows - 1) / kMoveRows, ((int64_t)1 << 20) / units), (int64_t)1);
   const dim3 grid((unsigned)blocks, a.c.num_kv_heads, a.b.n_seqs);
   if (a.dst_table) return launch_one(f, grid, 256, stream, a);
