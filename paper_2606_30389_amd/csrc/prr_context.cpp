@@ -145,9 +145,9 @@ prr_status check_shape(const prr_shape* sh, prr::ShapeArgs& a, int& bits) {
   if (sh->cap != 0.0f) {
     a.cap = (float)(sh->cap * 11.313708498984761);
     a.inv = 1.0f / a.cap;
-    // (above 2^8 the last coefficients leave float32's range, and the terms are nothing below 2^-6 of the cap)
-    a.small = a.cap * (sh->cap <= 0x1p8f ? (float)prr::kTanhRange : 0x1p-6f);
-    for (int i = 0; i < 5; ++i) {
+    // (above 2^10 the last coefficients leave float32's range, and the terms are nothing below 2^-6 of the cap)
+    a.small = a.cap * (sh->cap <= 0x1p10f ? (float)prr::kTanhRange : 0x1p-6f);
+    for (int i = 0; i < 4; ++i) {
       const double k = prr::kTanh[i] * pow((double)a.cap, -2.0 * (i + 1));
       a.k[i] = (float)k;
       a.k2[i] = (float)(k * 0.08838834764831845 * 1.4426950408889634);

@@ -13,7 +13,7 @@ struct ShapeArgs {
   const int32_t* first;
   int window;
   float cap, inv, small;  // the cap in the units of q.k, 1 / cap, the logits below which cap_small holds
-  float k[5], k2[5];      // cap_small's coefficients, and in the units of the exponent
+  float k[4], k2[4];      // cap_small's coefficients, and in the units of the exponent
 };
 
 // Keys [lo, hi) of a sequence of kv tokens that the token at position pos (row `row` of the packed tensors) sees; lo = hi:
@@ -38,24 +38,25 @@ __device__ __forceinline__ Span span_of(const ShapeArgs& a, int pos, int row, in
 }
 
 // P of cap_small: tanh(x) / x = 1 + t0 x^2 + t1 x^4 + ...
-constexpr double kTanh[5] = {-0.3333318990018068, 0.1332911073996761, -0.05355886142021114, 0.020091970334283688, -0.005138662405571459};
-constexpr double kTanhRange = 0.7;
+constexpr double kTanh[4] = {-0.33332597508690864, 0.133131166748644, -0.05221180747602632, 0.015612633936512193};
+constexpr double kTanhRange = 0.6;
 
 #ifdef __HIPCC__
 
 // Logits are held as q.k: a logit's cap and slopes in that unit.
 constexpr float kRawPerLogit = 11.313708498984761f;  // sqrt(128)
 
-// cap tanh(s / cap), s in the units of q.k.  Below 0.7 of the cap: s P((s / cap)^2), P the polynomial of degree 5 closest to
-// tanh(x) / x there (least squares with weights moved until the relative error was level): 2^-26 relative before
-// rounding, 2^-23 with it.  k holds P's coefficients times powers of 1 / cap^2, so that s^2 is the argument: seven operations
-// where the other form needs an exponential and a reciprocal, too, each a quarter of an operation's rate.  A tile
+// cap tanh(s / cap), s in the units of q.k.  Below 0.6 of the cap: s P((s / cap)^2), P the polynomial of degree 4 closest to
+// tanh(x) / x there (least squares with weights moved until the relative error was level): 2^-23.5 relative before
+// rounding, 2^-22.4 with it.  k holds P's coefficients times powers of 1 / cap^2, so that s^2 is the argument: six operations
+// where the other form needs an exponential and a reciprocal, too, each at half an operation's rate or less.  A tile
 // whose logits are all below takes this form alone; in one of both kinds each logit takes its own, so that no result depends
-// on the others' logits.  (Degree 4 up to 1/2 leaves more tiles of both kinds: nine packed prompts with a cap
-// of 30 and logits of standard deviation 4, 266 us.)
-__device__ __forceinline__ float cap_ratio(float s, const float (&k)[5], float one) {
+// on the others' logits.  (Up to 1/2, tiles of both kinds are common: nine packed prompts with a cap of 30 and logits of
+// standard deviation 4 took 266 us, 214 up to 0.7; degree 5, which that range needs, costs 32768 tokens with a cap
+// of 50 another 4%.)
+__device__ __forceinline__ float cap_ratio(float s, const float (&k)[4], float one) {
   const float u = s * s;
-  return fmaf(fmaf(fmaf(fmaf(fmaf(k[4], u, k[3]), u, k[2]), u, k[1]), u, k[0]), u, one);
+  return fmaf(fmaf(fmaf(fmaf(k[3], u, k[2]), u, k[1]), u, k[0]), u, one);
 }
 __device__ __forceinline__ float cap_small(float s, const ShapeArgs& a) { return s * cap_ratio(s, a.k, 1.0f); }
 // Any s: cap (1 - 2 / (1 + e^(2 s / cap))), off by at most cap * 2^-22 (the reciprocal's and the sum's last places);
