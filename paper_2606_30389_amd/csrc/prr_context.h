@@ -128,7 +128,6 @@ struct CompactLaunch {
   BatchArgs b;
   int budget, dst_stride;
   int stage_rows;  // of a sequence and KV head: no more can move
-  int phase;  // 0: to other pages, 1: to the stage, 2: from the stage
   bool e4m3;
 };
 

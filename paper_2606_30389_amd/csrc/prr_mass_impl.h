@@ -19,6 +19,12 @@ namespace {
 // itself; lanes are joined once, at the end.  So no weight moves, and the order of every sum is fixed: parts of the rows are
 // other workgroups' and are added by mass_join_kernel.
 //
+// Bound by the SIMDs: their matrix and vector instructions hardly overlap (256 cycles of products and 271 of multiply-adds,
+// exponentials and additions, what 16 rows x 64 keys take, are 468 together at two waves a SIMD, 428 at four).  8191 tokens of
+// float16, 32 / 8 heads, 320 us without a cap, 0.86 PFLOP/s, and 425 to 465 with one; 32 tokens over 131072, 32 / 2 heads, 49 to
+// 56 us, of which 13 are the keys'.  32x32x16 products overlap better (390) but leave no registers for the next rows'
+// products under these rows' weights: 7% slower; three waves a SIMD spill, 25% slower; two blocks a wave 3 to 9%.
+//
 // Every 32 tiles a lane's sums go to a second set, so that a sum of n rows is off by about (128 + n / 2048) 2^-24 at most.
 constexpr int kRows = 64;                 // rows of a tile
 constexpr int kFlush = 32;
