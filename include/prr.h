@@ -457,7 +457,8 @@ prr_status prr_decode_attn_shaped(const prr_dims* dims, const prr_batch* batch, 
  *   pages, page_count, cap  as for prr_decode_attn (one token per sequence then, cu_q NULL): only tokens of
  *                listed pages are written; or NULL
  *   mass_in      device [Hkv][max_pages][page_size] float32, or NULL = 0 (decay is not used then)
- *   mass_out     the same, out; may be mass_in.  Laid out as the cache is: a token's mass lies where its rows lie
+ *   mass_out     the same, out; may be mass_in.  Laid out as the cache is: a token's mass lies where its rows lie.  No
+ *                two sequences may share a page of it, what is no token of theirs is left as it was
  * Sums are float32 in a fixed order: the same call gives the same bits.  List and table entries out of range are
  * skipped.  Workspace: prr_mass_workspace_size bytes (cap 0 = no lists), 256-byte aligned, contents of no account
  * before and after (NULL if that is 0). */
@@ -475,7 +476,7 @@ prr_status prr_key_mass(const prr_dims* dims, const prr_batch* batch, const prr_
  *   budget       >= 1; sink, recent >= 0, sink + recent <= budget
  *   keep         device [n_seqs][Hkv][budget] int32 out: positions, ascending; entries behind the kept ones are left as
  *                they were
- *   kept_len     device [n_seqs] int32 out: min(budget, kv_len)
+ *   kept_len     device [n_seqs] int32 out: min(budget, kv_len); not the batch's kv_len itself
  * A token whose page-table entry is out of range has mass NaN.  Workspace: prr_keep_workspace_size bytes, as above. */
 size_t prr_keep_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t budget);
 prr_status prr_keep_tokens(const prr_dims* dims, const prr_batch* batch, const float* mass, int32_t budget, int32_t sink,

@@ -550,6 +550,8 @@ prr_status prr_keep_tokens(const prr_dims* dims, const prr_batch* batch, const f
   PRR_TRY(prr::api_check_ptr(mass, "mass", 16));
   PRR_TRY(prr::api_check_ptr(keep, "keep", 4));
   PRR_TRY(prr::api_check_ptr(kept_len, "kept_len", 4));
+  if (kept_len == batch->kv_len)  // (other workgroups still read it, and prr_cache_compact needs both)
+    return api_fail(PRR_ERR_INVALID_ARG, "kept_len is the batch's kv_len");
   PRR_TRY(check_ws(workspace, ws_bytes, keep_bytes(a)));
   a.mass = mass;
   a.keep = keep;

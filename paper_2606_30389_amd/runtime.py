@@ -317,7 +317,8 @@ class PagedCache:
               shape: Optional[Shape] = None):
         """The attention weight that each cached token received from the new tokens (their last `last` ones, 0 = all), whose
         attention gave m and l, on top of decay * before: float32 [Hkv][pages][page_size], laid out as the cache.  out: a
-        given one, `before` itself among them.  With lists only tokens of listed pages are written."""
+        given one, `before` itself among them.  Only the batch's tokens are written, with lists those of listed pages; the
+        others have what they had in `before` (0 without)."""
         self._check_batch(batch, q)
         for x, name in ((m, "m"), (l, "l")):
             _check(x, name, q.shape[:2], torch.float32, self.k.device)
@@ -329,7 +330,8 @@ class PagedCache:
         nbytes = L.prr_mass_workspace_size(self.dims, batch.native, shape, self.kind, last, cap)
         if out is None:
             with _stream_context(stream, self.k.device):
-                out = torch.zeros(self.k.shape[:3], dtype=torch.float32, device=self.k.device)
+                # (tokens that the call does not write keep what they had)
+                out = torch.zeros(self.k.shape[:3], dtype=torch.float32, device=self.k.device) if before is None else before.clone()
         L.prr_key_mass(self.dims, batch.native, shape, q, self.kind, self.k, self.k_scale, m, l, last, pages, counts, cap, before,
                        decay, out, self._workspace(nbytes, stream), nbytes, stream)
         return out

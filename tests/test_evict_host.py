@@ -110,7 +110,7 @@ def mass(P, d=None, b=None, shape=None, **over):
 
 
 def keep(P, d=None, b=None, **over):
-    a = dict(mass=FAKE, budget=20, sink=4, recent=5, keep=FAKE, kept_len=FAKE, workspace=FAKE, ws_bytes=1 << 40, stream=0)
+    a = dict(mass=FAKE, budget=20, sink=4, recent=5, keep=FAKE, kept_len=2 * FAKE, workspace=FAKE, ws_bytes=1 << 40, stream=0)
     a.update(over)
     return lambda: P.prr_keep_tokens(d or dims(P), b or batch(P), **a)
 
@@ -199,7 +199,7 @@ def test_mass_refusals(P):
 def test_keep_refusals(P):
     bad = P.PRR_ERR_INVALID_ARG
     for over in (dict(mass=None), dict(mass=FAKE + 8), dict(budget=0), dict(budget=2 ** 30 + 1), dict(sink=-1), dict(recent=-1), dict(sink=16),
-                 dict(recent=2 ** 31 - 1), dict(keep=None), dict(keep=FAKE + 2), dict(kept_len=None)):
+                 dict(recent=2 ** 31 - 1), dict(keep=None), dict(keep=FAKE + 2), dict(kept_len=None), dict(kept_len=FAKE)):  # (kv_len)
         _expect(P, bad, keep(P, **over))
     d, b = dims(P, max_pages=1 << 13), batch(P, max_kv=100000, table_stride=1 << 13)
     need = P.prr_keep_workspace_size(d, b, 20)

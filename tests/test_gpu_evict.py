@@ -544,6 +544,31 @@ def test_a_layer_that_evicts_and_decodes():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lists", [False, True])
+def test_tokens_outside_a_call_keep_their_mass(lists):
+    """A call for one sequence, or with lists, on top of the mass of a pool: the others' is in the result as it was."""
+    from paper_2606_30389_amd import runtime as R
+    cfg = R.PathConfig(num_q_heads=8, num_kv_heads=2, page_size=16, num_tokens=128, k_select=1)
+    cache = R.PagedCache(cfg, DEV, k=rand(2, 8, 16, S.D), v=rand(2, 8, 16, S.D, seed=1))
+    table = torch.tensor([[5, 2, 7, 0]], dtype=torch.int32, device=DEV)
+    q, batch = rand(1, 8, S.D, seed=2), R.Batch(DEV, [1], [50], table)
+    given = dict(pages=torch.tensor([[[1, 0], [3, 2]]], dtype=torch.int32, device=DEV),
+                 counts=torch.tensor([[1, 2]], dtype=torch.int32, device=DEV)) if lists else {}
+    _, _, m, l = cache.attend(batch, q, **given)
+    before = torch.rand(2, 8, 16, device=DEV)
+    was = before.clone()
+    got = cache.weigh(batch, q, m, l, before=before, decay=0.5, **given)
+    torch.cuda.synchronize()
+    written = torch.zeros(2, 8, 16, dtype=torch.bool)
+    for h, logical in enumerate([[1], [3, 2]] if lists else [range(4)] * 2):
+        for lp in logical:
+            written[h, int(table[0, lp]), :min(16, 50 - 16 * lp)] = True
+    got, was = got.cpu(), was.cpu()
+    assert torch.equal(before.cpu(), was) and torch.equal(got[~written], was[~written])
+    assert abs(float((got[written] - 0.5 * was[written]).sum()) - 8.0) < 1e-3  # (8 heads of weight one)
+
+
+@pytest.mark.gpu
 def test_eviction_on_other_streams_and_in_graphs():
     """weigh, keep and compact on a stream of their own, and captured: the results of the eager calls."""
     from paper_2606_30389_amd import runtime as R
