@@ -119,7 +119,7 @@ __device__ __forceinline__ void attend_tile(const TileData<E4M3>& d, const u32x4
   for (int i = 0; i < 4; ++i) {
     const bool live = 4 * j + i < valid && (!SHAPE || 4 * j + i >= skip);
     if constexpr (E4M3) s[i] *= __uint_as_float(((d.ks >> (8 * i)) & 0xffu) << 23);
-    if constexpr (SHAPE & kShapeCap) s[i] = cap_any(s[i], sh);
+    if constexpr (SHAPE & kShapeCap) s[i] = cap_exact(s[i], sh);
     if constexpr (SHAPE & kShapeSlopes) s[i] = fmaf(-slope, (float)(back - 4 * j - i), s[i]);
     s[i] = live ? s[i] : kNegInf;
     top = fmaxf(top, s[i]);

@@ -69,6 +69,9 @@ __device__ __forceinline__ float cap_any(float s, const ShapeArgs& a) {
   return fabsf(s) < a.small ? cap_small(s, a) : cap_large(s, a);
 }
 
+// Where memory bounds the kernel: the function itself, to its last places.
+__device__ __forceinline__ float cap_exact(float s, const ShapeArgs& a) { return a.cap * tanhf(s * a.inv); }
+
 // Exponents of weights relative to ref: log2(e) z / sqrt(128) - ref of capped logits, with the change of units in k2, so that
 // the product with s is the exponent's.  near: every logit of the caller's is below a.small.
 __device__ __forceinline__ float cap_exponent(float s, float ref, float scale2, bool near, const ShapeArgs& a) {
