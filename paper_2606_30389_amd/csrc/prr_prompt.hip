@@ -11,15 +11,29 @@ void plan_prompt(PromptLaunch& a) {
   }
   // Parts of a row tile's keys.  Fewer workgroups than CUs: as many parts, of at least eight tiles, as fill
   // the chip once (509 new of 65536 tokens, 28 / 4 heads: 460 us in four parts, 1403 in one; twice as many small
-  // ones fill it better, but joining them and power take that back: 472 in nine).
+  // ones fill it better, but joining them and power take that back: 472 in nine).  With a shape, two workgroups of four waves
+  // on a CU (four sequences of 500 new and up to 20000 tokens, window 2000, cap: 71 us, 79 with one, 75 of eight waves).
   // Enough workgroups, but so few that one sequence with many more keys than the others could outlast them
   // all: parts of 512 tiles, eight at most, for 2% where the lengths are alike (16 new tokens of 64 sequences, one of 131072 tokens
   // and 63 of 500, 32 / 8 heads: 2812 us in one part, 766 in four).
   const auto parts_of = [&](int64_t units) -> int64_t {
-    if (units <= 256) return max((int64_t)1, min(256 / max(units, (int64_t)1), key_tiles / 8));
+    const int64_t fill = a.shape && a.waves == 4 ? 512 : 256;
+    if (units <= fill) return max((int64_t)1, min(fill / max(units, (int64_t)1), key_tiles / 8));
     return units < 4096 ? min((key_tiles + 511) / 512, (int64_t)8) : 1;
   };
+  // Waves of a workgroup.  Four, and two workgroups a CU, start and end under each other's work; eight in turns keep the matrix
+  // cores busier over many tiles.  With a cap the softmax outlasts the products, and turns gain less: nine packed prompts
+  // with a window of 1024 tokens and a cap 214 us with four, 230 with eight, 2047 tokens with a cap 78, 95; 8192 tokens 705, 701.
+  // Without, 2047 tokens 62, 65; two of 12000 with a window of 2000 642, 622.  Where eight waves make fewer workgroups
+  // than CUs, four do up to 48 tiles (2500 tokens, 16 / 4 heads, 76, 90; 4000 79, 79; 8 x 160 over 4000 138, 132) and with
+  // documents, most of whose parts are empty (5163 tokens, 5 / 1 heads, eight documents, 62, 72); rows that eight waves
+  // would not fill by half always do (16 new of 65536 tokens, 32 / 8 heads, 70, 103).
   a.waves = key_tiles <= 16 ? 4 : 8;
+  if (a.shape) {
+    const int64_t rows = (int64_t)a.b.max_q * a.group;
+    const bool few = rows * a.b.n_seqs * a.num_kv_heads <= 256 * 256;
+    if (key_tiles <= (a.shape & kShapeCap ? 64 : few ? 48 : 32) || rows <= 128 || (few && a.sh.first)) a.waves = 4;
+  }
   a.magic = a.group == 1 ? 0u : (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
   const int rows = 32 * a.waves;
   const int64_t per = ((int64_t)a.b.max_q * a.group + rows - 1) / rows, each = a.b.n_seqs * per;

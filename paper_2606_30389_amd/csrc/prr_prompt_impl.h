@@ -40,7 +40,7 @@ namespace {
 //
 // Up to 1024 tokens, four waves a workgroup, two workgroups a CU, which start and end (about 9 us a
 // workgroup) under each other's work instead of taking turns: 32 sequences of 512 tokens, 32 / 8 heads, 140 us
-// (eight waves: 152), 1024 tokens 29 (39); 2048 tokens 61 (58), 16384 tokens 2118 (1916).
+// (eight waves: 152), 1024 tokens 29 (39); 2048 tokens 61 (58), 16384 tokens 2118 (1916).  (plan_prompt: with a shape.)
 //
 // SHAPE (prr_shape.h): a row sees an interval of keys, [lo, hi).  The workgroup's tiles are those that its rows'
 // intervals touch; a tile that every row of a wave sees whole takes the path without comparisons.  Caps and slopes

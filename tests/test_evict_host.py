@@ -166,10 +166,11 @@ def test_windows_bound_the_workspaces(P):
     few = dict(n_seqs=1, max_kv=1 << 16, table_stride=1 << 12)
     p, t = batch(P, total_q=4, max_q=4, **few), one(P, total_q=1, **few)
     plain = P.prr_prompt_workspace_size(d, p)
-    assert plain == P.prr_prompt_shaped_workspace_size(d, p, None) == P.prr_prompt_shaped_workspace_size(d, p, P.make_shape(cap=5.0))
-    assert 0 < P.prr_prompt_shaped_workspace_size(d, p, P.make_shape(window=5000)) < plain
+    assert plain == P.prr_prompt_shaped_workspace_size(d, p, None) == P.prr_prompt_shaped_workspace_size(d, p, P.make_shape())
+    whole = P.prr_prompt_shaped_workspace_size(d, p, P.make_shape(cap=5.0))
+    assert 0 < P.prr_prompt_shaped_workspace_size(d, p, P.make_shape(window=5000)) < whole
     assert P.prr_prompt_shaped_workspace_size(d, p, P.make_shape(window=100)) == 0
-    assert P.prr_prompt_shaped_workspace_size(d, p, P.make_shape(window=5000, prefix=FAKE)) == plain
+    assert P.prr_prompt_shaped_workspace_size(d, p, P.make_shape(window=5000, prefix=FAKE)) == whole
     plain = P.prr_decode_workspace_size(d, t, 0)
     assert plain == P.prr_decode_shaped_workspace_size(d, t, None, 0) > P.prr_decode_shaped_workspace_size(d, t, P.make_shape(window=5000), 0) > 0
     sh = P.make_shape(window=5000)
