@@ -15,7 +15,7 @@
  * whole caches, prr_cache_read gives e4m3 pages back in 16 bits.  prr_prompt_attn_shaped and
  * prr_decode_attn_shaped do the same with capped, biased and masked scores.  A cache is made
  * smaller by prr_key_mass (the attention weight that each token received), prr_keep_tokens (which
- * stay) and prr_cache_compact (their rows to their new places).
+ * stay) and prr_cache_compact (their rows to their new places); prr_mass_clear makes places ready for new tokens.
  *
  * Citations name sections, equations and the appendix of "Predict, Reuse, and
  * Repair: Accelerating Dynamic Sparse Attention for Long-Context LLM Decoding".
@@ -456,7 +456,8 @@ prr_status prr_decode_attn_shaped(const prr_dims* dims, const prr_batch* batch, 
  *   last         only the last so many new tokens of a sequence count; 0 = all
  *   pages, page_count, cap  as for prr_decode_attn (one token per sequence then, cu_q NULL): only tokens of
  *                listed pages are written; or NULL
- *   mass_in      device [Hkv][max_pages][page_size] float32, or NULL = 0 (decay is not used then)
+ *   mass_in      device [Hkv][max_pages][page_size] float32, or NULL = 0 (decay is not used then).  0 for a token that
+ *                received none yet (prr_mass_clear)
  *   mass_out     the same, out; may be mass_in.  Laid out as the cache is: a token's mass lies where its rows lie.  No
  *                two sequences may share a page of it, what is no token of theirs is left as it was
  * Sums are float32 in a fixed order: the same call gives the same bits.  List and table entries out of range are
@@ -468,6 +469,16 @@ prr_status prr_key_mass(const prr_dims* dims, const prr_batch* batch, const prr_
                         const void* k_cache, const uint8_t* k_scale, const float* m, const float* l, int32_t last,
                         const int32_t* pages, const int32_t* page_count, int32_t cap, const float* mass_in, float decay,
                         float* mass_out, void* workspace, size_t ws_bytes, hipStream_t stream);
+
+/* The mass of places that hold no token yet, or none any more: 0 at positions [from_len, kv_len) of every sequence and KV
+ * head, and behind them on the last page that has any of its tokens.
+ *   batch        its kv_len and page table (the new tokens do not matter)
+ *   from_len     device [n_seqs] int32, cut to [0, kv_len]; may be the batch's kv_len itself
+ *   mass         device [Hkv][max_pages][page_size] float32 in and out
+ * A token's mass_in is 0 before it received any, which is the caller's to see to: prr_cache_compact leaves the mass of the
+ * places that it vacates, and a page that a pool gives to a sequence has what its last owner left there.  Table entries out
+ * of range are skipped.  No workspace. */
+prr_status prr_mass_clear(const prr_dims* dims, const prr_batch* batch, const int32_t* from_len, float* mass, hipStream_t stream);
 
 /* Which tokens stay: of every sequence and KV head min(budget, kv_len), the first `sink` and the last `recent` among
  * them, the others those of the largest mass (equal ones: the lower position; NaN below everything).
@@ -491,7 +502,8 @@ prr_status prr_keep_tokens(const prr_dims* dims, const prr_batch* batch, const f
  *   dst_table    device [n_seqs][dst_stride] int32: the pages of the places, none of which may be a page that a sequence
  *                of the batch has; or NULL = the sequences' own pages (in place, none of which two sequences may share)
  *   dst_stride   >= ceil(min(budget, max_kv) / page_size) with dst_table
- * What is not such a place is left as it was.  Positions outside [0, kv_len) and table entries out of range are skipped.
+ * What is not such a place is left as it was, the mass of vacated places among it: prr_mass_clear before tokens are appended
+ * there (in place: from kept_len; with dst_table: a batch of dst_table and kept_len, from kept_len).  Positions outside [0, kv_len) and table entries out of range are skipped.
  * The tokens are in their order still, but at other positions: prr_rope_append's `positions` gives later tokens the
  * rotation of their true ones.  Workspace: prr_compact_workspace_size bytes in place, none otherwise; as above. */
 size_t prr_compact_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t kv_kind, int32_t budget,

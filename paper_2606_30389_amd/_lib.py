@@ -60,7 +60,8 @@ EXPORTED = (
     "prr_rope_freqs", "prr_rope_append", "prr_cache_read", "prr_prompt_workspace_size", "prr_prompt_attn",
     "prr_decode_workspace_size", "prr_decode_attn",
     "prr_prompt_shaped_workspace_size", "prr_prompt_attn_shaped", "prr_decode_shaped_workspace_size", "prr_decode_attn_shaped",
-    "prr_mass_workspace_size", "prr_key_mass", "prr_keep_workspace_size", "prr_keep_tokens", "prr_compact_workspace_size",
+    "prr_mass_workspace_size", "prr_key_mass", "prr_mass_clear", "prr_keep_workspace_size", "prr_keep_tokens",
+    "prr_compact_workspace_size",
     "prr_cache_compact",
 )
 
@@ -159,6 +160,7 @@ _SIGS = {
     "prr_decode_attn_shaped": (_I, [_DIMS, _BATCH, _SHAPE, _P, _I, _P, _P, _P, _P, _P, _P, _I, _P, _P, _P, _P, _P, _S, _P]),
     "prr_mass_workspace_size": (_S, [_DIMS, _BATCH, _SHAPE, _I, _I, _I]),
     "prr_key_mass": (_I, [_DIMS, _BATCH, _SHAPE, _P, _I, _P, _P, _P, _P, _I, _P, _P, _I, _P, _F, _P, _P, _S, _P]),
+    "prr_mass_clear": (_I, [_DIMS, _BATCH, _P, _P, _P]),
     "prr_keep_workspace_size": (_S, [_DIMS, _BATCH, _I]),
     "prr_keep_tokens": (_I, [_DIMS, _BATCH, _P, _I, _I, _I, _P, _P, _P, _S, _P]),
     "prr_compact_workspace_size": (_S, [_DIMS, _BATCH, _I, _I, _I]),
@@ -445,6 +447,10 @@ def prr_key_mass(dims, batch, shape, q, kv_kind, k_cache, k_scale, m, l, last, p
     _on_device(_lib.prr_key_mass, q, stream, ctypes.byref(dims), ctypes.byref(batch), _shape(shape), _ptr(q), kv_kind,
                _ptr(k_cache), _ptr(k_scale), _ptr(m), _ptr(l), last, _ptr(pages), _ptr(page_count), cap, _ptr(mass_in), decay,
                _ptr(mass_out), _ptr(workspace), ws_bytes)
+
+
+def prr_mass_clear(dims, batch, from_len, mass, stream=None):
+    _on_device(_lib.prr_mass_clear, mass, stream, ctypes.byref(dims), ctypes.byref(batch), _ptr(from_len), _ptr(mass))
 
 
 def prr_keep_workspace_size(dims, batch, budget) -> int:

@@ -536,6 +536,24 @@ prr_status prr_key_mass(const prr_dims* dims, const prr_batch* batch, const prr_
   return hip_status(prr::launch_mass(a, stream), "key mass");
 }
 
+prr_status prr_mass_clear(const prr_dims* dims, const prr_batch* batch, const int32_t* from_len, float* mass, hipStream_t stream) {
+  prr::MassClearLaunch a;
+  PRR_TRY(check_heads(dims));
+  PRR_TRY(check_batch(dims, batch));
+  PRR_TRY(prr::api_check_ptr(from_len, "from_len", 4));
+  PRR_TRY(prr::api_check_ptr(mass, "mass", 4));
+  memset(&a, 0, sizeof(a));
+  a.mass = mass;
+  a.from = from_len;
+  a.b = batch_args(batch);
+  a.num_kv_heads = dims->num_kv_heads;
+  a.max_pages = dims->max_pages;
+  a.page_size = dims->page_size;
+  a.page_shift = log2_of(dims->page_size);
+  if (a.b.max_kv == 0) return api_ok();  // (no sequence has a token)
+  return hip_status(prr::launch_mass_clear(a, stream), "mass clear");
+}
+
 size_t prr_keep_workspace_size(const prr_dims* dims, const prr_batch* batch, int32_t budget) {
   prr::KeepLaunch a;
   if (plan(dims, batch, budget, 0, 0, a) != PRR_OK) return 0;

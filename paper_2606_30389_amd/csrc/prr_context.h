@@ -118,6 +118,13 @@ struct KeepLaunch {
   int chunks, chunk;  // workgroups of a sequence and KV head, tokens of each
 };
 
+struct MassClearLaunch {
+  float* mass;
+  const int32_t* from;
+  BatchArgs b;
+  int num_kv_heads, max_pages, page_size, page_shift;
+};
+
 struct CompactLaunch {
   CacheArgs c;
   float* mass;  // or null
@@ -146,6 +153,7 @@ __host__ __device__ inline int64_t keep_words(const KeepLaunch& a) {
   return (2048 * (int64_t)a.chunks + 64 + 4 + 2 * (int64_t)a.chunks * a.chunk + 63) / 64 * 64;
 }
 hipError_t launch_keep(const KeepLaunch& a, hipStream_t stream);
+hipError_t launch_mass_clear(const MassClearLaunch& a, hipStream_t stream);
 // bytes of the stage of a call in place
 size_t compact_stage_bytes(const CompactLaunch& a);
 hipError_t launch_compact(const CompactLaunch& a, hipStream_t stream);

@@ -493,7 +493,27 @@ __global__ __launch_bounds__(256) void compact_kernel(const CompactLaunch a) {
   }
 }
 
+// The mass of places without a token: positions from `from` to the end of the sequence's last page, one thread a position.
+// Memory and the launch bound it: 32 sequences of up to 16384 tokens, 8 KV heads, to 2048: 7.5 us;
+// one of 5000 to 1000 4.0.
+__global__ __launch_bounds__(256) void mass_clear_kernel(const MassClearLaunch a) {
+  const int h = blockIdx.y, s = blockIdx.z;
+  const int kv = min(max(a.b.kv_len[s], 0), a.b.max_kv);
+  const int from = min(max(a.from[s], 0), kv);
+  const int64_t end = ((int64_t)kv + a.page_size - 1) >> a.page_shift << a.page_shift;
+  for (int64_t p = from + (int64_t)blockIdx.x * 256 + threadIdx.x; p < end; p += (int64_t)gridDim.x * 256) {
+    const int phys = phys_page(a.b.page_table, a.b.table_stride, a.max_pages, s, (int)(p >> a.page_shift));
+    if (phys >= 0) a.mass[(((int64_t)h * a.max_pages + phys) << a.page_shift) + (p & (a.page_size - 1))] = 0.0f;
+  }
+}
+
 }  // namespace
+
+hipError_t launch_mass_clear(const MassClearLaunch& a, hipStream_t stream) {
+  const int64_t units = (int64_t)a.b.n_seqs * a.num_kv_heads;
+  const int64_t blocks = max(min(((int64_t)a.b.max_kv + a.page_size + 255) / 256, ((int64_t)1 << 18) / units), (int64_t)1);
+  return launch_one((const void*)mass_clear_kernel, dim3((unsigned)blocks, a.num_kv_heads, a.b.n_seqs), 256, stream, a);
+}
 
 void plan_keep(KeepLaunch& a) {
   a.chunks = 1;

@@ -358,7 +358,9 @@ class PagedCache:
 
     def compact(self, batch: Batch, keep, kept_len, mass=None, dst_table=None, stream=None):
         """The kept tokens (keep's results) to the beginnings of their sequences, on the sequences' own pages or on those of
-        dst_table ([sequence][pages]); with them their mass.  The batch's lengths are the caller's to change (kept_len)."""
+        dst_table ([sequence][pages]); with them their mass, and 0 behind them, up to the end of the page that ends the
+        sequence there, for tokens that are appended next (a page beyond, given to a sequence later, is its owner's to clear).
+        The batch's lengths are the caller's to change (kept_len)."""
         self._check_batch(batch, None)
         n = batch.native.n_seqs
         _check(keep, "keep", (n, self.cfg.num_kv_heads, keep.shape[-1]), torch.int32, self.k.device)
@@ -372,6 +374,10 @@ class PagedCache:
         L.prr_cache_compact(self.dims, batch.native, keep, kept_len, budget, self.kind, self.k, self.v, self.k_scale, self.v_scale,
                             mass, dst_table, 0 if dst_table is None else dst_table.shape[-1], self._workspace(nbytes, stream),
                             nbytes, stream)
+        if mass is not None:
+            places = batch.native if dst_table is None else L.make_batch(
+                n, n, 1, min(budget, batch.native.max_kv), None, kept_len, dst_table, dst_table.shape[-1])
+            L.prr_mass_clear(self.dims, places, kept_len, mass, stream)
 
     def evict(self, batch: Batch, mass, budget, sink=0, recent=0, dst_table=None, stream=None):
         """keep and compact: the cache holds at most `budget` tokens of each sequence.  Returns how many ([sequence], on the
@@ -500,7 +506,7 @@ class LayerState:
         cfg, cache = self.cfg, self.cache()
         batch = self._one(batch, q.shape[0], stream)
         mass = cache.weigh(batch, q, m, l, last=last, stream=stream, shape=shape)
-        cache.evict(batch, mass, budget, sink, recent, stream=stream)
+        cache.compact(batch, *cache.keep(batch, mass, budget, sink, recent, stream=stream), stream=stream)
         kept = min(budget, cfg.num_tokens)
         L.prr_build_page_meta(self.dims, self.k, self.page_table, kept, 0, -(-kept // cfg.page_size), self.meta, stream)
         with _stream_context(stream, self.k.device):
