@@ -145,8 +145,8 @@ prr_status check_shape(const prr_shape* sh, prr::ShapeArgs& a, int& bits) {
   if (sh->cap != 0.0f) {
     a.cap = (float)(sh->cap * 11.313708498984761);
     a.inv = 1.0f / a.cap;
-    // (above 2^10 the last coefficients leave float32's range, and the terms are nothing below 2^-6 of the cap)
-    a.small = a.cap * (sh->cap <= 0x1p10f ? (float)prr::kTanhRange : 0x1p-6f);
+    a.small = a.cap * (float)prr::kTanhRange;
+    a.wide = sh->cap > prr::kMostCap;
     for (int i = 0; i < 4; ++i) {
       const double k = prr::kTanh[i] * pow((double)a.cap, -2.0 * (i + 1));
       a.k[i] = (float)k;
@@ -154,7 +154,7 @@ prr_status check_shape(const prr_shape* sh, prr::ShapeArgs& a, int& bits) {
     }
     bits |= prr::kShapeCap;
   }
-  if (sh->slopes) bits |= prr::kShapeSlopes;
+  if (sh->slopes || a.wide) bits |= prr::kShapeSlopes;  // (those instances take NULL for slopes of 0)
   if (bits || sh->window || sh->prefix || sh->first) bits |= prr::kShapeSpan;
   return PRR_OK;
 }

@@ -229,7 +229,7 @@ __global__ __launch_bounds__(NW * kWave) void decode_kernel(const DecodeLaunch a
   const int tiles = key_tiles(a, s, h, lo, kv), parts = max(parts_of(a, tiles), 1);
   if (part >= parts) return;
   float slope = 0.0f;
-  if constexpr (SHAPE & kShapeSlopes) slope = a.sh.slopes[h * G + min(n, G - 1)] * kRawPerLogit;
+  if constexpr (SHAPE & kShapeSlopes) slope = slope_of<SHAPE>(a.sh, h * G + min(n, G - 1));
 
   u32x4_t qf[4];
   const uint16_t* q = static_cast<const uint16_t*>(a.q) + ((int64_t)(s * a.c.num_kv_heads + h) * G + min(n, G - 1)) * kHeadDim;

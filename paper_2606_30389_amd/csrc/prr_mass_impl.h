@@ -190,7 +190,7 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(const MassLaunch a) {
         for (int x = 0; x < 4; ++x) offset[x] = at((t >> 4) + 16 * x, tok, head) * (2 * kHeadDim) + 16 * (t & 15);
         if (t < kRows) {
           info = at(t, r_tok, head);
-          if constexpr (SHAPE & kShapeSlopes) r_slope = a.sh.slopes[h * G + head] * kRawPerLogit;
+          if constexpr (SHAPE & kShapeSlopes) r_slope = slope_of<SHAPE>(a.sh, h * G + head);
         }
       }
       const int64_t row = ((int64_t)(sq.q0 + i0 + tok0) * a.c.num_kv_heads + h) * G;
@@ -258,7 +258,7 @@ __global__ __launch_bounds__(256, 2) void mass_kernel(const MassLaunch a) {
 #pragma unroll
           for (int b = 0; b < KB; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) d[b][i] = cap_any(d[b][i], a.sh);
+            for (int i = 0; i < 4; ++i) d[b][i] = cap_wide(d[b][i], a.sh);
         }
       }
       if constexpr (SHAPE & kShapeSlopes) {

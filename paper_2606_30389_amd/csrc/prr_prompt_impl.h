@@ -168,7 +168,7 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
     all1 = hi_first / kTokens;
     ntiles = (keys + kTokens - 1) / kTokens;
     t0 = min(min(lo, keys) / kTokens + part * a.part_tiles, ntiles);
-    if constexpr (SHAPE & kShapeSlopes) slope = a.sh.slopes[h * G + head] * kRawPerLogit;
+    if constexpr (SHAPE & kShapeSlopes) slope = slope_of<SHAPE>(a.sh, h * G + head);
   } else {
     const int wave_lo = first + over_group(min(row0 + 32 * w, rows - 1), a.magic);
     keys = max(0, first + over_group(min(row0 + kRows - 1, rows - 1), a.magic) + 1);
@@ -302,7 +302,12 @@ __global__ __launch_bounds__(NW * kWave, 2) void prompt_kernel(const PromptLaunc
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(sc[b][i]));
-      if (__all(most < a.sh.small)) {
+      if ((SHAPE & kShapeSlopes) && a.sh.wide) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[b][i] = cap_wide(sc[b][i], a.sh);
+      } else if (__all(most < a.sh.small)) {
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
