@@ -451,8 +451,8 @@ prr_status prr_decode_attn_shaped(const prr_dims* dims, const prr_batch* batch, 
  *   shape        of the scores z, as in the attention that gave m and l, or NULL: causal, plain
  *   q            device [total_q][Hq][128] dtype
  *   kv_kind, k_cache, k_scale  the keys (scales: E4M3 only)
- *   m, l         device [total_q][Hq] float32, as prr_prompt_attn, prr_decode_attn or prr_repair gave them.  A token
- *                with l = 0 gives no weight
+ *   m, l         device [total_q][Hq] float32, as prr_prompt_attn, prr_decode_attn or prr_repair gave them.  A row
+ *                with l = 0 gives no weight, whatever its query and m hold
  *   last         only the last so many new tokens of a sequence count; 0 = all
  *   pages, page_count, cap  as for prr_decode_attn (one token per sequence then, cu_q NULL): only tokens of
  *                listed pages are written; or NULL
