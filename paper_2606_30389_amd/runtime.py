@@ -316,9 +316,10 @@ class PagedCache:
     def weigh(self, batch: Batch, q, m, l, before=None, decay=1.0, last=0, pages=None, counts=None, out=None, stream=None,
               shape: Optional[Shape] = None):
         """The attention weight that each cached token received from the new tokens (their last `last` ones, 0 = all), whose
-        attention gave m and l, on top of decay * before: float32 [Hkv][pages][page_size], laid out as the cache.  out: a
-        given one, `before` itself among them.  Only the batch's tokens are written, with lists those of listed pages; the
-        others have what they had in `before` (0 without)."""
+        attention gave m and l, on top of decay * before: float32 [Hkv][pages][page_size], laid out as the cache.  Only
+        the batch's tokens are written, with lists those of listed pages.  out: a given one, `before` itself among them,
+        whose other tokens are left as they were, whatever `before` holds for them (so that batches of one pool can share
+        it); None: a new one, in which they have what they had in `before` (0 without)."""
         self._check_batch(batch, q)
         for x, name in ((m, "m"), (l, "l")):
             _check(x, name, q.shape[:2], torch.float32, self.k.device)

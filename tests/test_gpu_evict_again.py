@@ -1,4 +1,4 @@
-"""Mass that goes on after an eviction."""
+"""Mass that goes on after an eviction, and in a buffer of one's own."""
 import pytest
 import torch
 
@@ -165,3 +165,26 @@ def test_mass_clear_at_its_borders(page):
         if n % page:
             was[:, int(b.d_table[s, n // page]), n % page:] = 0.0
     assert torch.equal(mass, was)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lists", [False, True])
+def test_mass_in_a_buffer_of_ones_own(lists):
+    """A given out that is not `before`: the call's tokens on top of `before`, all else as it was in out."""
+    from paper_2606_30389_amd import runtime as R
+    cfg = R.PathConfig(num_q_heads=8, num_kv_heads=2, page_size=16, num_tokens=128, k_select=1)
+    cache = R.PagedCache(cfg, DEV, k=rand(2, 8, 16, S.D), v=rand(2, 8, 16, S.D, seed=1))
+    table = torch.tensor([[5, 2, 7, 0]], dtype=torch.int32, device=DEV)
+    q, batch = rand(1, 8, S.D, seed=2), R.Batch(DEV, [1], [50], table)
+    given = dict(pages=torch.tensor([[[1, 0], [3, 2]]], dtype=torch.int32, device=DEV),
+                 counts=torch.tensor([[1, 2]], dtype=torch.int32, device=DEV)) if lists else {}
+    _, _, m, l = cache.attend(batch, q, **given)
+    before, out = torch.rand(2, 8, 16, device=DEV), 9.0 + torch.rand(2, 8, 16, device=DEV)
+    want, was = cache.weigh(batch, q, m, l, before=before, decay=0.5, **given), out.clone()
+    got = cache.weigh(batch, q, m, l, before=before, decay=0.5, out=out, **given)
+    torch.cuda.synchronize()
+    written = torch.zeros(2, 8, 16, dtype=torch.bool, device=DEV)
+    for h, logical in enumerate([[1], [3, 2]] if lists else [range(4)] * 2):
+        for lp in logical:
+            written[h, int(table[0, lp]), :min(16, 50 - 16 * lp)] = True
+    assert got is out and torch.equal(got[written], want[written]) and torch.equal(got[~written], was[~written])
