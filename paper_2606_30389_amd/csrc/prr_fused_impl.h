@@ -102,10 +102,12 @@ __device__ __forceinline__ void put_rep(uint64_t* base, int h, int k, uint32_t v
 }
 
 // The threshold record of KV head h (words 0: T, 1: mode | tie cut << 2) and the missed
-// count, published in every copy (one thread).
-__device__ __forceinline__ void publish_thr(const FusedLaunch& a, int h, uint32_t T, uint32_t me, uint32_t epoch) {
-  put_rep(a.t_thr, h, 0, T, epoch);
-  put_rep(a.t_thr, h, 1, me, epoch);
+// count, published in every copy (one thread).  "Every candidate" (mode 1) is published as the
+// candidates' smallest key: those who read it hold pages that may be no candidates (where exactly as
+// many pages as are selected reach the candidates' bound, all others lie below it).
+__device__ __forceinline__ void publish_thr(const FusedLaunch& a, int h, const SelThreshold& th, int eq_cut, uint32_t epoch) {
+  put_rep(a.t_thr, h, 0, th.T, epoch);
+  put_rep(a.t_thr, h, 1, (th.mode == 0 ? 0u : 2u) | ((uint32_t)eq_cut << 2), epoch);
   stamp(a, kStampThreshold);
 }
 __device__ __forceinline__ void publish_mcnt(const FusedLaunch& a, int h, uint32_t v, uint32_t epoch) {
@@ -1082,13 +1084,13 @@ __device__ __forceinline__ void select_finish(const FusedLaunch& a, uint32_t ep,
   const SelThreshold th = sel2_threshold<kFT, J>(key, cand, a.kextra_a, L.sel);
   const bool early = th.mode != 2 || th.need_eq >= th.eq_total;
   if (prr && early && t == 0) {
-    publish_thr(a, h, th.T, (uint32_t)th.mode | ((uint32_t)kEqAll << 2), ep);
+    publish_thr(a, h, th, kEqAll, ep);
   }
   const uint64_t inA = sel2_membership<kFT, J>(key, page, cand, force, th, &L.eq_cut, L.sel);
   if (prr && !early) {
     __syncthreads();
     if (t == 0) {
-      publish_thr(a, h, th.T, (uint32_t)th.mode | ((uint32_t)L.eq_cut << 2), ep);
+      publish_thr(a, h, th, L.eq_cut, ep);
     }
   }
 
@@ -1215,7 +1217,7 @@ __device__ __forceinline__ void select_wave(const FusedLaunch& a, uint32_t ep, i
     if (prr && !early) {
       eq_cut = __builtin_amdgcn_readfirstlane(wave_umin((uint32_t)eq_cut));
       if (lane == 0) {
-        publish_thr(a, h, th.T, (uint32_t)th.mode | ((uint32_t)eq_cut << 2), ep);
+        publish_thr(a, h, th, eq_cut, ep);
       }
     }
     // pages of late speculation: flagged, within the late capacity, never in P^t
@@ -1409,7 +1411,7 @@ __device__ __forceinline__ void role_select(const FusedLaunch& a, uint32_t ep, i
     const SelThreshold th = bsel_threshold<kFT>(k2, c2, a.kextra_a, L.bsel);
     const bool early = th.mode != 2 || th.need_eq >= th.eq_total;
     if (a.schedule == 1 && t == 0 && early) {
-      publish_thr(a, h, th.T, (uint32_t)th.mode | ((uint32_t)kEqAll << 2), ep);
+      publish_thr(a, h, th, kEqAll, ep);
     }
     const int nM = early ? miss_block(a, ep, h, c.total, th, k2, L) : -1;
     select_wave<BF16, PS>(a, ep, h, c.total, qn, th, nM, U);
@@ -1625,7 +1627,7 @@ __device__ __forceinline__ uint32_t keep_in_A(const FusedLaunch& a, uint32_t ep,
   for (int k = 0; k < NPW; ++k) {
     if (pg[k] < 0 || page_forced(a, pg[k])) continue;
     const uint32_t key = score_key(__uint_as_float(sc[k]));
-    const bool in = mode == 1 || (mode == 2 && (key > T || (key == T && pg[k] <= eq_cut)));
+    const bool in = mode && (key > T || (key == T && pg[k] <= eq_cut));
     if (!in) keep &= ~(1u << k);
   }
   return keep;
@@ -1659,7 +1661,7 @@ __device__ __forceinline__ void keep_fold_publish(const FusedLaunch& a, int slot
     const uint32_t T = (uint32_t)v0, me = (uint32_t)v1;
     const int mode = (int)(me & 3u), eq_cut = (int)(me >> 2);
     const uint32_t key = score_key(__uint_as_float(sc));
-    const bool in = p >= 0 && (page_forced(a, p) || mode == 1 || (mode == 2 && (key > T || (key == T && p <= eq_cut))));
+    const bool in = p >= 0 && (page_forced(a, p) || (mode && (key > T || (key == T && p <= eq_cut))));
     const uint32_t m = (uint32_t)__ballot(in) & ((1u << kFW) - 1u);
     if (lane == 0) L.kmask = m;
   }

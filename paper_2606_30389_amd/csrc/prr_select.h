@@ -30,7 +30,7 @@ struct Sel2Lds {
 
 struct SelThreshold {
   int mode;       // 0: no candidate taken, 1: every candidate, 2: candidates above T and ties
-  uint32_t T;
+  uint32_t T;     // mode 1: the smallest key of a candidate
   int need_eq;    // keys equal to T to take, in page order
   int eq_total;   // keys equal to T among the candidates
 };
@@ -91,6 +91,7 @@ __device__ __forceinline__ SelThreshold sel2_threshold(const uint32_t (&key)[J],
   if (kextra <= 0 || cnt == 0) return r;
   if (kextra >= cnt) {
     r.mode = 1;
+    r.T = lo;
     return r;
   }
   r.mode = 2;
@@ -337,6 +338,7 @@ __device__ __forceinline__ SelThreshold wsel_threshold(const uint32_t (&key)[NK]
   if (kextra <= 0 || cnt == 0) return r;
   if (kextra >= cnt) {
     r.mode = 1;
+    r.T = lo;
     return r;
   }
   r.mode = 2;
@@ -540,6 +542,7 @@ __device__ __forceinline__ SelThreshold bsel_threshold(const uint32_t (&key)[2],
   if (kextra <= 0 || cnt == 0) return r;
   if (kextra >= cnt) {
     r.mode = 1;
+    r.T = lo;
     return r;
   }
   r.mode = 2;
