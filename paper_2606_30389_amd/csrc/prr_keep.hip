@@ -411,7 +411,7 @@ __global__ __launch_bounds__(kThreads) void keep_write_kernel(const KeepLaunch a
 // is one copy.  In place rows move towards the beginning, over rows that others still have to read: all of them go to
 // a stage first, and from there to their places.  A workgroup takes 64 rows, a thread 16 bytes of a row at a time, its
 // loads before its stores; memory bounds it.  What is not a stage passes the caches by: 32 sequences of 2048 e4m3 tokens,
-// 8 KV heads, from cold memory 59 us, 4.6 TB/s (68 by way of the caches); in place 94.
+// 8 KV heads, from cold memory 59 us, 4.6 TB/s (68 by way of the caches); in place 94 to 101.
 constexpr int kMoveRows = 64;
 
 // PHASE 0: to other pages, 1: to the stage, 2: from the stage

@@ -11,7 +11,8 @@ namespace prr {
 namespace {
 
 // mass[j] = decay before[j] + sum over (token, query head) rows of exp(z_j - m) / l, with m and l of the attention that the
-// rows have had.  With log2(l) in the exponent a weight is one multiply-add and one exponential of a logit.
+// rows have had.  With log2(l) in the exponent a weight is one multiply-add and one exponential of a logit (off by 4.0e-7 for 32
+// tokens over 131072, where a division by l is off by 1.3e-7).
 //
 // A workgroup of four waves takes 64 KB keys of one sequence and KV head, a wave 16 KB of them, which stay in registers, and
 // walks over the rows that see any of them, 64 at a time through LDS (two buffers, the next rows' loads in flight during a
@@ -21,8 +22,9 @@ namespace {
 //
 // Bound by the SIMDs: their matrix and vector instructions hardly overlap (256 cycles of products and 271 of multiply-adds,
 // exponentials and additions, what 16 rows x 64 keys take, are 468 together at two waves a SIMD, 428 at four).  8191 tokens of
-// float16, 32 / 8 heads, 320 us without a cap, 0.86 PFLOP/s, and 425 to 465 with one; 32 tokens over 131072, 32 / 2 heads, 49 to
-// 56 us, of which 13 are the keys'.  32x32x16 products overlap better (390) but leave no registers for the next rows'
+// float16, 32 / 8 heads, 315 us without a cap, 0.88 PFLOP/s, and 425 to 465 with one, e4m3 keys 3% more (with a cap and slopes
+// their four blocks take all 256 registers and spill 2); 32 tokens over 131072, 32 / 2 heads, 49 to 58 us, of which 13 are the
+// keys'.  32x32x16 products overlap better (390) but leave no registers for the next rows'
 // products under these rows' weights: 7% slower; three waves a SIMD spill, 25% slower; two blocks a wave 3 to 9%.
 //
 // Every 32 tiles a lane's sums go to a second set, so that a sum of n rows is off by about (128 + n / 2048) 2^-24 at most.

@@ -101,7 +101,9 @@ class Rope:
 class Shape:
     """What a layer does to its scores (prr_shape): a tanh cap, a bias that falls with the distance (slopes: float32 [heads]),
     and which keys a token sees: a window back from it, none before its document's beginning (first: int32 [rows]), and the
-    sequence's prefix (prefix: int32 [sequences])."""
+    sequence's prefix (prefix: int32 [sequences]).  Distances, windows and these numbers count places in the cache, so after
+    an eviction they are not those of the text: a layer with slopes or a window gets shorter ones.  The decode step
+    (select, repair, DecodeStack) knows no shapes: single tokens of such a layer take PagedCache.attend."""
 
     def __init__(self, cap=0.0, slopes=None, window=0, first=None, prefix=None):
         self.slopes, self.first, self.prefix = slopes, first, prefix
@@ -478,7 +480,8 @@ class LayerState:
                 shape: Optional[Shape] = None, positions=None, q_out=None):
         """The last len(q) of the cfg.num_tokens tokens: into the cache, their causal attention (or that of a shape), and the
         metadata of the pages that they touch.  q [n][Hq][128], k, v [n][Hkv][128]; returns (o, m, l), in a given q_out the
-        rotated queries.  positions: the tokens' true ones, after an eviction.  A given batch holds
+        rotated queries.  positions: the tokens' true ones, after an eviction.  The shape is this call's alone: select, repair
+        and the decode step attend plainly.  A given batch holds
         this one sequence, of cfg.num_tokens tokens; its rows may be more than its new tokens."""
         cfg = self.cfg
         batch = self._one(batch, q.shape[0], stream)
@@ -502,7 +505,8 @@ class LayerState:
               shape: Optional[Shape] = None):
         """The cache with at most `budget` of the cfg.num_tokens tokens: the first `sink`, the last `recent`, and those that
         received the most attention from the last new tokens, whose rotated queries q [n][Hq][128] and statistics m, l a
-        prefill gave.  Metadata is built anew, predictions start anew.  Returns the tokens that stay, which
+        prefill gave (not mass that was added up before: that takes cache().evict, then what this method does after it).
+        Metadata is built anew, predictions start anew.  Returns the tokens that stay, which
         DecodeStack.set_tokens makes the layers' length once all of them are evicted to it."""
         cfg, cache = self.cfg, self.cache()
         batch = self._one(batch, q.shape[0], stream)
