@@ -62,7 +62,7 @@ def test_steps_after_an_eviction(schedule):
         if schedule in ("TWO_STREAM", "FUSED_PRR"):
             stack.step(P.PRR_SCHED_PREFILL if schedule == "TWO_STREAM" else P.PRR_SCHED_FUSED_PREFILL, s)
         steps(3)
-        # the prompt's last tokens judge again what is there by now
+        # the prompt's last tokens decide again over what is there by now
         stack.set_tokens(n)
         stack.set_tokens(st.evict(*stats, 300, sink=4, recent=50, last=32))
         steps(20)
